@@ -359,6 +359,83 @@ int dt_commit(void *stream, int batch, int n_layers, dt_dtype t, int Hkv, int D,
               int32_t *new_prefix_len, int32_t *next_root_token);
 
 /*
+ * What rows of logits say of tokens: log-probabilities of given tokens, entropy, the k best alternatives -- for the tokens
+ * that a step has emitted (row_of = path_nodes, tokens = out_tokens of dt_accept), or for a text that is scored.
+ * Entry (b, s), s < per_seq, of sequence b goes by row x = row b*rows_per_seq + row_of[b, s] of the logits (row_of NULL: row
+ * b*rows_per_seq + s, per_seq <= rows_per_seq); with z = x / temperature, over the V tokens:
+ *   logprob     [batch, per_seq]    z_y - log sum exp z for y = tokens[b, s]; 0 if y is outside 0 .. V-1
+ *   entropy     [batch, per_seq]    -sum q log q, q = softmax(z)                     (may be NULL)
+ *   stats       [batch, per_seq, 2] the largest logit m of the row, as it is, and log sum exp((x - m) / temperature): what the
+ *                                   gradient goes by; log sum exp z is their sum where temperature is 1
+ *   top_logprob [batch, per_seq, k] log-probabilities of the k largest logits, best first, and
+ *   top_id      [batch, per_seq, k] their tokens; equal logits by ascending id; slots beyond the finite entries (-inf, -1)
+ * logprob may be NULL, tokens too then; k = 0 takes no alternatives (top_logprob and top_id are not looked at).  An entry whose
+ * row_of is outside 0 .. rows_per_seq-1 has no row: 0, 0, (0, 0), slots (-inf, -1), and reads nothing.  Two entries may go by
+ * one row.  Logits of -inf are tokens of probability 0; a row that has no other has log-probabilities -inf, entropy 0
+ * and stats (-inf, -inf).  Sums are fp32, relative to the row's largest logit.
+ * Workspace: dt_logprob_workspace_bytes(batch*per_seq, V) bytes.
+ * Errors: null logits or stats, logprob without tokens, per_seq > rows_per_seq without row_of, a temperature outside 1e-4 .. 1e4, k > 0 without
+ * its outputs, pointers not aligned to their elements -> DT_ERR_INVALID_ARG; k > min(DT_K_MAX, V), V > DT_VOCAB_MAX or more than
+ * 2^24 - 1 entries -> DT_ERR_LIMIT.
+ */
+#define DT_VOCAB_MAX 524288
+int dt_logprob_workspace_bytes(int64_t n_rows, int V, size_t *bytes);
+int dt_token_logprobs(void *stream, int batch, int per_seq, const void *logits, dt_dtype t, int V, int64_t row_stride,
+                      int64_t rows_per_seq, const int32_t *row_of, const int32_t *tokens, float temperature, int k,
+                      float *logprob, float *entropy, float *stats, float *top_logprob, int32_t *top_id, void *ws,
+                      size_t ws_bytes);
+
+/*
+ * The gradient of both in the logits, row r of n_rows: with q, H and the temperature as above, y = tokens[r],
+ *     grad[r, j] = ( grad_logprob[r] (1[j = y] - q_j) - grad_entropy[r] q_j (log q_j + H) ) / temperature
+ *   stats, entropy             as written by dt_token_logprobs (entropy may be NULL without grad_entropy)
+ *   grad_logprob, grad_entropy [n_rows], either may be NULL: 0 (tokens too, without grad_logprob).  A row whose token
+ *                              is outside 0 .. V-1 has no log-probability and takes nothing from grad_logprob.
+ *   grad                       [n_rows, grad_stride] type t, all V entries of every row are written; its rows may be the
+ *                              logits' own (same pointer, same stride), else they must not overlap them
+ * One rounding, to type t, at the end.  Errors as above; a grad that is the logits with another stride, a grad_logprob without tokens or a
+ * grad_entropy without entropy -> DT_ERR_INVALID_ARG.
+ */
+int dt_token_logprobs_grad(void *stream, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride,
+                           const int32_t *tokens, float temperature, const float *stats, const float *entropy,
+                           const float *grad_logprob, const float *grad_entropy, void *grad, int64_t grad_stride);
+
+/*
+ * The loss by which a draft model learns the target's answers: rows of its logits against a teacher's best tokens (the
+ * top_logprob / top_id of dt_token_logprobs, or the top_val / top_id / lse of dt_topk_rows), with its gradient.
+ * Row r of the logits goes by row teacher_row[r] of the teacher (NULL: row r), whose entries i < k are token
+ * teacher_id[., i] with log p_i = teacher_val[., i] - teacher_lse[.] (teacher_lse NULL: 0); an entry whose token is outside 0 .. V-1 or whose
+ * value is -inf is none.  With q = softmax(row / temperature), S the set of the entries' tokens, P = sum p_i:
+ *   loss[r] = sum_i p_i (log p_i - log q_i)                                    (forward Kullback-Leibler divergence)
+ *     DT_DISTILL_TAIL    + p_t (log p_t - log q_t), p_t = max(0, 1 - P), q_t = sum of q outside S: what the teacher gives to
+ *                          all other tokens together
+ *     DT_DISTILL_RENORM  with p_i / P in the place of p_i                        (not both)
+ *   stats [n_rows, 2]  as in dt_token_logprobs
+ *   tail  [n_rows]     log q_t
+ *   grad  [n_rows, grad_stride], may be NULL: type t, grad_loss[r] (NULL: 1) times the gradient of loss[r] in the logits; its rows may be the
+ *                      logits' own (same pointer, same stride), else they must not overlap them
+ * A row whose teacher_row is outside 0 .. n_teacher-1 has no teacher: loss, stats and tail 0, gradient 0.  Several rows may have the same
+ * teacher.  A token that is in several entries counts with the sum of its terms.  A student's probability of 0 where the teacher has
+ * some makes the loss +inf; such a row's gradient is that of the formula, with q of a row without finite entries 0.
+ * The teacher's probabilities are taken in 64 bits, sums over the row are fp32, one rounding of the gradient to type t.
+ * dt_distill_rows_grad is the gradient on its own, from the stats and tail that dt_distill_rows has written for the same arguments.
+ * Workspace: dt_logprob_workspace_bytes(n_rows, V) bytes.
+ * Errors: k < 1, fewer teacher rows than rows without teacher_row, unknown or both flags, a temperature outside 1e-4 .. 1e4, a grad that is the logits
+ * with another stride -> DT_ERR_INVALID_ARG; k > DT_DISTILL_K_MAX, V > DT_VOCAB_MAX or more than 2^24 - 1 rows -> DT_ERR_LIMIT.
+ */
+#define DT_DISTILL_K_MAX 128
+#define DT_DISTILL_TAIL 1
+#define DT_DISTILL_RENORM 2
+int dt_distill_rows(void *stream, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride, int k,
+                    int64_t n_teacher, const float *teacher_val, const int32_t *teacher_id, const float *teacher_lse,
+                    const int32_t *teacher_row, float temperature, int flags, const float *grad_loss, float *loss, float *stats,
+                    float *tail, void *grad, int64_t grad_stride, void *ws, size_t ws_bytes);
+int dt_distill_rows_grad(void *stream, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride, int k,
+                         int64_t n_teacher, const float *teacher_val, const int32_t *teacher_id, const float *teacher_lse,
+                         const int32_t *teacher_row, float temperature, int flags, const float *grad_loss, const float *stats,
+                         const float *tail, void *grad, int64_t grad_stride);
+
+/*
  * Optional per-kernel timing, for measurement only (off by default; not part of the step).
  * dt_profile_enable(n > 0) pre-creates n HIP event pairs and switches timing on: every kernel
  * launched by the calls above then carries an event pair on its dispatch that records the
@@ -366,7 +443,7 @@ int dt_commit(void *stream, int batch, int n_layers, dt_dtype t, int Hkv, int D,
  * dt_profile_enable(0) switches it off.  dt_profile_read sums, for one kernel id
  * (0 draft row chunks, 1 row merge, 2 tree, 3 attention, 4 reserved (no launch), 5 target row
  * chunks, 6 accept, 7 dt_topk_rows chunks, 8 commit, 9 policy layer 1, 10 policy head, 11 per-node target samples,
- * 12 reward), the elapsed milliseconds of the launches recorded
+ * 12 reward, 13 token log-probabilities, 14 their join, 15 distillation loss, 16 its join, 17 gradients of rows), the elapsed milliseconds of the launches recorded
  * since the last enable, waiting for them to finish.  Not thread-safe.
  */
 int dt_profile_enable(int max_launches);

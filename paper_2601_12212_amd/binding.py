@@ -14,6 +14,8 @@ DT_TT_MAX, DT_D_MAX, DT_K_MAX, DT_MASK_WORDS = 128, 8, 32, 2
 DT_F32, DT_BF16 = 0, 1
 DT_TREE_EARLY_STOP = 1
 DT_ACCEPT_GREEDY, DT_ACCEPT_STOCHASTIC, DT_ACCEPT_SAMPLED = 0, 1, 2
+DT_VOCAB_MAX, DT_DISTILL_K_MAX = 524288, 128
+DT_DISTILL_TAIL, DT_DISTILL_RENORM = 1, 2
 
 _lib = None
 _call = None
@@ -67,6 +69,11 @@ def load_library():
         lib.dt_reward_step.argtypes = [vp, i32, vp, i32, f32, vp, vp, vp, vp, vp, vp]
         lib.dt_reward_step.restype = i32
         lib.dt_commit.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, i32, vp, vp]
+        lib.dt_logprob_workspace_bytes.argtypes = [i64, i32, C.POINTER(sz)]
+        lib.dt_token_logprobs.argtypes = [vp, i32, i32, vp, i32, i32, i64, i64, vp, vp, f32, i32] + [vp] * 6 + [sz]
+        lib.dt_token_logprobs_grad.argtypes = [vp, i64, vp, i32, i32, i64, vp, f32] + [vp] * 5 + [i64]
+        lib.dt_distill_rows.argtypes = [vp, i64, vp, i32, i32, i64, i32, i64] + [vp] * 4 + [f32, i32] + [vp] * 5 + [i64, vp, sz]
+        lib.dt_distill_rows_grad.argtypes = [vp, i64, vp, i32, i32, i64, i32, i64] + [vp] * 4 + [f32, i32] + [vp] * 4 + [i64]
         lib.dt_profile_enable.argtypes = [i32]
         lib.dt_profile_enable.restype = i32
         lib.dt_profile_read.argtypes = [i32, C.POINTER(C.c_double), C.POINTER(i32)]
@@ -76,7 +83,8 @@ def load_library():
         lib.dt_init.argtypes = []
         for fn in ("dt_init", "dt_workspace_bytes", "dt_topk_rows", "dt_build_tree", "dt_tree_attention", "dt_accept", "dt_commit",
                    "dt_level_state_bytes", "dt_expand_level", "dt_finish_tree", "dt_action_table",
-                   "dt_policy_workspace_bytes", "dt_policy_step"):
+                   "dt_policy_workspace_bytes", "dt_policy_step", "dt_logprob_workspace_bytes", "dt_token_logprobs", "dt_token_logprobs_grad",
+                   "dt_distill_rows", "dt_distill_rows_grad"):
             getattr(lib, fn).restype = i32
         _lib = lib
     return _lib
@@ -236,6 +244,46 @@ def dt_commit(dtype_of, Hkv, D, k_tree_ptrs, v_tree_ptrs, k_prefix_ptrs, v_prefi
                                      new_prefix_len, next_root_token)
     if rc:
         raise DtError("dt_commit", rc)
+
+
+def dt_logprob_workspace_bytes(n_rows, V):
+    out = C.c_size_t(0)
+    _check("dt_logprob_workspace_bytes", load_library().dt_logprob_workspace_bytes(n_rows, V, C.byref(out)))
+    return out.value
+
+
+def dt_token_logprobs(logits, row_of, tokens, temperature, k, logprob, entropy, stats, top_logprob, top_id, ws):
+    """logits [B, rows, V]; row_of (None: entry s by row s) and tokens int32 [B, n]; logprob, entropy [B, n], stats [B, n, 2], top_logprob and
+    top_id [B, n, k].  Tensors of the row operators are on the current device, outputs and indices contiguous; what is not
+    raises."""
+    rc = (_call or _native()).token_logprobs(logits, row_of, tokens, temperature, k, logprob, entropy, stats, top_logprob, top_id, ws)
+    if rc:
+        raise DtError("dt_token_logprobs", rc)
+
+
+def dt_token_logprobs_grad(logits, tokens, temperature, stats, entropy, grad_logprob, grad_entropy, grad):
+    """logits and grad [n, V], the others [n], stats [n, 2]."""
+    rc = (_call or _native()).token_logprobs_grad(logits, tokens, temperature, stats, entropy, grad_logprob, grad_entropy, grad)
+    if rc:
+        raise DtError("dt_token_logprobs_grad", rc)
+
+
+def dt_distill_rows(logits, teacher_val, teacher_id, teacher_lse, teacher_row, temperature, flags, grad_loss, loss, stats, tail, grad,
+                    ws):
+    """logits and grad (None: the loss alone) [n, V]; teacher_val and teacher_id [m, k], teacher_lse [m] or None, teacher_row int32 [n] or
+    None; grad_loss (None: 1), loss and tail [n], stats [n, 2]."""
+    rc = (_call or _native()).distill_rows(logits, teacher_val, teacher_id, teacher_lse, teacher_row, temperature, flags, grad_loss, loss,
+                                           stats, tail, grad, ws)
+    if rc:
+        raise DtError("dt_distill_rows", rc)
+
+
+def dt_distill_rows_grad(logits, teacher_val, teacher_id, teacher_lse, teacher_row, temperature, flags, grad_loss, stats, tail, grad):
+    """The gradient alone, from the stats and tail of dt_distill_rows."""
+    rc = (_call or _native()).distill_rows_grad(logits, teacher_val, teacher_id, teacher_lse, teacher_row, temperature, flags, grad_loss,
+                                                stats, tail, grad)
+    if rc:
+        raise DtError("dt_distill_rows_grad", rc)
 
 
 def dt_profile_enable(max_launches):

@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdt.so")
 PYCALL = os.path.join(HERE, "_dtcall.so")
-SOURCES = ["api.cpp", "profile.cpp", "rows.hip", "tree.hip", "attention.hip", "accept.hip", "commit.hip", "policy.hip"]
+SOURCES = ["api.cpp", "profile.cpp", "rows.hip", "tree.hip", "attention.hip", "accept.hip", "commit.hip", "policy.hip", "logprobs.hip", "distill.hip"]
 WAITING = ["rows.hip", "attention.hip"]   # kernels whose workgroups wait for each other
 BUILD = os.path.join(HERE, "_build")
 LIB_SHORT, PYCALL_SHORT = os.path.join(BUILD, "libdt_short_waits.so"), os.path.join(BUILD, "_dtcall.so")

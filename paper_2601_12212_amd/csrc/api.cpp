@@ -540,4 +540,130 @@ int dt_commit(void *stream, int batch, int n_layers, dt_dtype t, int Hkv, int D,
     return DT_OK;
 }
 
+// ---- rows of logits: log-probabilities, losses, gradients ----
+namespace {
+constexpr int64_t VOCAB_ROWS_MAX = (1 << 24) - 1;  // 256 threads to a row and 2^32 - 1 threads to a launch
+inline bool bad_temperature(float t) { return !(t >= 1e-4f && t <= 1e4f); }
+inline bool bad_rows(const void *p, dt_dtype t) { return !p || (uintptr_t)p % (t == DT_BF16 ? 2 : 4); }
+inline bool bad_words(const void *p) { return !p || (uintptr_t)p % 4; }
+inline bool bad_words_or_null(const void *p) { return (uintptr_t)p % 4 != 0; }
+// the gradient's rows lie in a memory of their own or are the logits' rows
+inline bool bad_grad(const void *grad, int64_t grad_stride, const void *logits, int64_t row_stride, int V, dt_dtype t) {
+    return bad_rows(grad, t) || grad_stride < V || (grad == logits && grad_stride != row_stride);
+}
+inline size_t logprob_ws(int64_t n, int V) {
+    const size_t a = dt::logprob_workspace(n, V), b = dt::distill_workspace(n, V);
+    return align_up(a > b ? a : b);
+}
+}  // namespace
+
+int dt_logprob_workspace_bytes(int64_t n_rows, int V, size_t *bytes) {
+    if (!bytes || n_rows < 0) return DT_ERR_INVALID_ARG;
+    if (V < 1 || V > DT_VOCAB_MAX || n_rows > VOCAB_ROWS_MAX) return DT_ERR_LIMIT;
+    *bytes = logprob_ws(n_rows, V) + 256;
+    return DT_OK;
+}
+
+int dt_token_logprobs(void *stream, int batch, int per_seq, const void *logits, dt_dtype t, int V, int64_t row_stride,
+                      int64_t rows_per_seq, const int32_t *row_of, const int32_t *tokens, float temperature, int k,
+                      float *logprob, float *entropy, float *stats, float *top_logprob, int32_t *top_id, void *ws,
+                      size_t ws_bytes) {
+    if (batch < 0 || per_seq < 0 || bad_dtype(t)) return DT_ERR_INVALID_ARG;
+    if (batch == 0 || per_seq == 0) return DT_OK;
+    if (bad_rows(logits, t) || bad_words(stats) || bad_words_or_null(row_of) || bad_words_or_null(tokens) ||
+        bad_words_or_null(logprob) || bad_words_or_null(entropy) || bad_words_or_null(top_logprob) || bad_words_or_null(top_id) ||
+        (logprob && !tokens) || row_stride < V || rows_per_seq < 1 || (!row_of && per_seq > rows_per_seq) || k < 0 ||
+        (k > 0 && (!top_logprob || !top_id)) || bad_temperature(temperature))
+        return DT_ERR_INVALID_ARG;
+    const int64_t n = (int64_t)batch * per_seq;
+    if (V < 1 || V > DT_VOCAB_MAX || k > DT_K_MAX || k > V || n > VOCAB_ROWS_MAX) return DT_ERR_LIMIT;
+    if (!ws || (uintptr_t)ws % 256 || ws_bytes < logprob_ws(n, V)) return DT_ERR_WORKSPACE;
+    dt::LogprobArgs a = {};
+    a.logits = logits; a.dtype = t; a.V = V; a.per_seq = per_seq; a.k = k; a.n = n;
+    a.row_stride = row_stride; a.rows_per_seq = rows_per_seq; a.row_of = row_of; a.tokens = tokens;
+    a.c = (float)(1.4426950408889634074 / (double)temperature);
+    a.logprob = logprob; a.entropy = entropy; a.stats = stats; a.top_logprob = top_logprob; a.top_id = top_id; a.ws = ws;
+    (void)hipGetLastError();  // a stale error left by another HIP user of this process is not ours
+    hipError_t e = dt::logprob_launch(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e);
+    return DT_OK;
+}
+
+int dt_token_logprobs_grad(void *stream, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride,
+                           const int32_t *tokens, float temperature, const float *stats, const float *entropy,
+                           const float *grad_logprob, const float *grad_entropy, void *grad, int64_t grad_stride) {
+    if (n_rows < 0 || bad_dtype(t)) return DT_ERR_INVALID_ARG;
+    if (n_rows == 0) return DT_OK;
+    if (bad_rows(logits, t) || bad_words(stats) || bad_words_or_null(tokens) || bad_words_or_null(entropy) ||
+        bad_words_or_null(grad_logprob) || bad_words_or_null(grad_entropy) || row_stride < V || (grad_logprob && !tokens) ||
+        (grad_entropy && !entropy) || bad_temperature(temperature) || bad_grad(grad, grad_stride, logits, row_stride, V, t))
+        return DT_ERR_INVALID_ARG;
+    if (V < 1 || V > DT_VOCAB_MAX || n_rows > VOCAB_ROWS_MAX) return DT_ERR_LIMIT;
+    dt::LogprobGradArgs a = {};
+    a.logits = logits; a.dtype = t; a.V = V; a.n = n_rows; a.row_stride = row_stride; a.grad_stride = grad_stride;
+    a.tokens = tokens; a.stats = stats; a.entropy = entropy; a.g_logprob = grad_logprob; a.g_entropy = grad_entropy;
+    a.c = (float)(1.4426950408889634074 / (double)temperature); a.inv_t = 1.0f / temperature; a.grad = grad;
+    (void)hipGetLastError();  // a stale error left by another HIP user of this process is not ours
+    hipError_t e = dt::logprob_grad_launch(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e);
+    return DT_OK;
+}
+
+// the checks that both calls of the distillation share, and their common arguments
+static int distill_args(dt::DistillArgs &a, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride, int k,
+                        int64_t n_teacher, const float *teacher_val, const int32_t *teacher_id, const float *teacher_lse,
+                        const int32_t *teacher_row, float temperature, int flags, const float *grad_loss, void *grad,
+                        int64_t grad_stride) {
+    if (bad_rows(logits, t) || row_stride < V || k < 1 || n_teacher < 0 || bad_words(teacher_val) || bad_words(teacher_id) ||
+        bad_words_or_null(teacher_lse) || bad_words_or_null(teacher_row) || bad_words_or_null(grad_loss) ||
+        bad_temperature(temperature) || (flags & ~(DT_DISTILL_TAIL | DT_DISTILL_RENORM)) ||
+        flags == (DT_DISTILL_TAIL | DT_DISTILL_RENORM) || (!teacher_row && n_teacher < n_rows) ||
+        (grad && bad_grad(grad, grad_stride, logits, row_stride, V, t)))
+        return DT_ERR_INVALID_ARG;
+    if (V < 1 || V > DT_VOCAB_MAX || k > DT_DISTILL_K_MAX || n_rows > VOCAB_ROWS_MAX) return DT_ERR_LIMIT;
+    a.logits = logits; a.dtype = t; a.V = V; a.k = k; a.flags = flags; a.n = n_rows; a.row_stride = row_stride;
+    a.grad_stride = grad_stride; a.n_teacher = n_teacher; a.teacher_val = teacher_val; a.teacher_lse = teacher_lse;
+    a.teacher_id = teacher_id; a.teacher_row = teacher_row; a.grad_loss = grad_loss; a.grad = grad;
+    a.c = (float)(1.4426950408889634074 / (double)temperature); a.inv_t = 1.0f / temperature;
+    return DT_OK;
+}
+
+int dt_distill_rows(void *stream, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride, int k,
+                    int64_t n_teacher, const float *teacher_val, const int32_t *teacher_id, const float *teacher_lse,
+                    const int32_t *teacher_row, float temperature, int flags, const float *grad_loss, float *loss, float *stats,
+                    float *tail, void *grad, int64_t grad_stride, void *ws, size_t ws_bytes) {
+    if (n_rows < 0 || bad_dtype(t)) return DT_ERR_INVALID_ARG;
+    if (n_rows == 0) return DT_OK;
+    dt::DistillArgs a = {};
+    if (int rc = distill_args(a, n_rows, logits, t, V, row_stride, k, n_teacher, teacher_val, teacher_id, teacher_lse, teacher_row,
+                              temperature, flags, grad_loss, grad, grad_stride))
+        return rc;
+    if (bad_words(loss) || bad_words(stats) || bad_words(tail)) return DT_ERR_INVALID_ARG;
+    if (!ws || (uintptr_t)ws % 256 || ws_bytes < logprob_ws(n_rows, V)) return DT_ERR_WORKSPACE;
+    a.loss = loss; a.stats = stats; a.tail = tail; a.ws = ws;
+    (void)hipGetLastError();  // a stale error left by another HIP user of this process is not ours
+    hipError_t e = dt::distill_launch(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e);
+    return DT_OK;
+}
+
+int dt_distill_rows_grad(void *stream, int64_t n_rows, const void *logits, dt_dtype t, int V, int64_t row_stride, int k,
+                         int64_t n_teacher, const float *teacher_val, const int32_t *teacher_id, const float *teacher_lse,
+                         const int32_t *teacher_row, float temperature, int flags, const float *grad_loss, const float *stats,
+                         const float *tail, void *grad, int64_t grad_stride) {
+    if (n_rows < 0 || bad_dtype(t)) return DT_ERR_INVALID_ARG;
+    if (n_rows == 0) return DT_OK;
+    dt::DistillArgs a = {};
+    if (!grad) return DT_ERR_INVALID_ARG;
+    if (int rc = distill_args(a, n_rows, logits, t, V, row_stride, k, n_teacher, teacher_val, teacher_id, teacher_lse, teacher_row,
+                              temperature, flags, grad_loss, grad, grad_stride))
+        return rc;
+    if (bad_words(stats) || bad_words(tail)) return DT_ERR_INVALID_ARG;
+    a.stats = const_cast<float *>(stats); a.tail = const_cast<float *>(tail);
+    (void)hipGetLastError();  // a stale error left by another HIP user of this process is not ours
+    hipError_t e = dt::distill_grad_launch(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e);
+    return DT_OK;
+}
+
 }  // extern "C"

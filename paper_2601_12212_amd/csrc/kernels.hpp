@@ -15,7 +15,8 @@ namespace dt {
 // of pre-created HIP events attached to its dispatch (hipExtLaunchKernelGGL), which record the
 // kernel's own begin and end; dt_profile_read sums the elapsed times per kernel id.
 enum KernelId { KID_ROWS_DRAFT = 0, KID_ROWS_MERGE, KID_TREE, KID_ATTN, KID_RESERVED_4 /* no launch; the others keep their numbers */, KID_ROWS_TARGET,
-                KID_ACCEPT, KID_ROWS_UNIFORM, KID_COMMIT, KID_POLICY_L1, KID_POLICY_HEAD, KID_NODE_SAMPLE, KID_REWARD, KID_COUNT };
+                KID_ACCEPT, KID_ROWS_UNIFORM, KID_COMMIT, KID_POLICY_L1, KID_POLICY_HEAD, KID_NODE_SAMPLE, KID_REWARD,
+                KID_LOGPROBS, KID_LOGPROBS_JOIN, KID_DISTILL, KID_DISTILL_JOIN, KID_ROWS_GRAD, KID_COUNT };
 bool prof_next(int kid, hipEvent_t *start, hipEvent_t *stop);  // false when timing is off
 
 template <typename F, typename... Args>
@@ -192,5 +193,53 @@ struct RewardArgs {
     int32_t *reward_steps, *interval_done;
 };
 hipError_t reward_launch(const RewardArgs &a, hipStream_t st);
+
+// ------------------------------------------------- log-probabilities of tokens (logprobs.hip)
+struct LogprobArgs {
+    const void *logits;
+    int dtype, V, per_seq, k;
+    int64_t n, row_stride, rows_per_seq;  // n entries, per_seq to a sequence
+    const int32_t *row_of, *tokens;       // [n], may be null
+    float c;                              // log2(e) / temperature
+    float *logprob, *entropy, *stats;     // the first two may be null
+    float *top_logprob;                   // [n, k]
+    int32_t *top_id;
+    void *ws;                             // sums of the parts of rows, then
+    unsigned long long *keys;             // [n, parts, k] their best
+    int parts, part_elems;                // set by the launch
+};
+size_t logprob_workspace(int64_t n, int V);
+hipError_t logprob_launch(LogprobArgs a, hipStream_t st);
+
+struct LogprobGradArgs {
+    const void *logits;
+    int dtype, V;
+    int64_t n, row_stride, grad_stride;
+    const int32_t *tokens;                                 // may be null, as either gradient may
+    const float *stats, *entropy, *g_logprob, *g_entropy;
+    float c, inv_t;
+    void *grad;
+    int parts, part_elems;
+};
+hipError_t logprob_grad_launch(LogprobGradArgs a, hipStream_t st);
+
+// ---------------------------------------------- loss against a teacher's best (distill.hip)
+struct DistillArgs {
+    const void *logits;
+    int dtype, V, k, flags;
+    int64_t n, row_stride, grad_stride, n_teacher;
+    const float *teacher_val, *teacher_lse;  // [n_teacher, k], [n_teacher] or null
+    const int32_t *teacher_id, *teacher_row; // [n_teacher, k], [n] or null
+    const float *grad_loss;                  // [n] or null: 1
+    float c, inv_t;
+    float *loss, *stats, *tail;
+    void *grad;                              // or null
+    void *ws;                                // sums of the parts of rows, then
+    float *s_elems;                          // [n, k] the student's logits of the teacher's tokens
+    int parts, part_elems;                   // set by the launch
+};
+size_t distill_workspace(int64_t n, int V);
+hipError_t distill_launch(DistillArgs a, hipStream_t st);
+hipError_t distill_grad_launch(DistillArgs a, hipStream_t st);  // reads stats and tail
 
 }  // namespace dt

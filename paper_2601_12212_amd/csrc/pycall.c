@@ -5,18 +5,21 @@
  * object cost another 5.5 us per call (2.8 of them the stream); here it is about 1 us.
  *
  * Every function takes the positional arguments of its namesake in binding.py and returns the dt_status as an int.
- * Tensors are anything with data_ptr(), shape, stride(), dtype and nbytes.  This module knows the interpreter and no torch; what
+ * Tensors are anything with data_ptr(), shape, stride(), dtype and nbytes (and, for the row operators, whose tensors are checked,
+ * numel(), is_contiguous() and device).  This module knows the interpreter and no torch; what
  * can be read without the interpreter goes through a reader that was built for the torch that is running (tensor_reader.cpp), if
  * set_reader() was given one.  The interpreter lock is released during the library call.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <string.h>
+
 #include "../../include/dt.h"
 #include "tensor_reader.h"
 
 static PyObject *g_f32, *g_bf16, *g_get_device, *g_get_stream;  /* set by setup() */
-static PyObject *s_data_ptr, *s_shape, *s_stride, *s_dtype, *s_nbytes;
+static PyObject *s_data_ptr, *s_shape, *s_stride, *s_dtype, *s_nbytes, *s_numel, *s_contiguous, *s_device, *s_type, *s_index;
 static PyObject *g_capsule;                                     /* set by set_reader(); holds the reader */
 static const dt_tensor_reader *g_reader;
 
@@ -96,10 +99,11 @@ static size_t nbytes(const dt_tensor_reader *rd, PyObject *t) {
     }
     return v;
 }
-/* torch's current stream on the current device */
-static void *stream(void) {
+/* torch's current stream on the current device, and that device */
+static void *stream_on(int *device) {
     void *p = NULL;
     PyObject *dev, *st;
+    *device = -1;
     if (PyErr_Occurred()) return NULL;
     if (!g_get_stream) {
         PyErr_SetString(PyExc_RuntimeError, "setup() has not been called");
@@ -107,10 +111,76 @@ static void *stream(void) {
     }
     dev = PyObject_CallNoArgs(g_get_device);
     st = dev ? PyObject_CallOneArg(g_get_stream, dev) : NULL;
+    if (dev) *device = inum(dev);
     if (st) p = PyLong_AsVoidPtr(st);
     Py_XDECREF(dev);
     Py_XDECREF(st);
     return p;
+}
+
+static void *stream(void) {
+    int device;
+    return stream_on(&device);
+}
+/* What the row operators ask of every tensor before its pointer goes to a kernel. */
+static void plain(const dt_tensor_reader *rd, PyObject *t, dt_tensor_plain *out) {
+    PyObject *r, *i;
+    memset(out, 0, sizeof *out);
+    if (PyErr_Occurred()) return;
+    if (rd && rd->plain(t, out)) return;
+    if ((r = PyObject_GetAttr(t, s_dtype)) != NULL) {
+        PyObject *name = PyObject_Str(r);
+        const char *c = name ? PyUnicode_AsUTF8(name) : NULL;
+        if (c) out->kind = r == g_f32 ? DT_KIND_F32 : r == g_bf16 ? DT_KIND_BF16 : !strcmp(c, "torch.int32") ? DT_KIND_I32 :
+                           !strcmp(c, "torch.uint8") ? DT_KIND_U8 : DT_KIND_OTHER;
+        Py_XDECREF(name);
+        Py_DECREF(r);
+    }
+    if (!PyErr_Occurred() && (r = PyObject_CallMethodNoArgs(t, s_numel)) != NULL) {
+        out->numel = num(r);
+        Py_DECREF(r);
+    }
+    if (!PyErr_Occurred() && (r = PyObject_CallMethodNoArgs(t, s_contiguous)) != NULL) {
+        out->contiguous = PyObject_IsTrue(r);
+        Py_DECREF(r);
+    }
+    if (!PyErr_Occurred() && (r = PyObject_GetAttr(t, s_device)) != NULL) {
+        PyObject *type = PyObject_GetAttr(r, s_type);
+        out->device = -1;
+        if (type && PyUnicode_Check(type) && !PyUnicode_CompareWithASCIIString(type, "cuda") && (i = PyObject_GetAttr(r, s_index)) != NULL) {
+            out->device = inum(i);
+            Py_DECREF(i);
+        }
+        Py_XDECREF(type);
+        Py_DECREF(r);
+    }
+}
+static void on_device(const char *name, const dt_tensor_plain *p, int device) {
+    if (!PyErr_Occurred() && p->device != device) PyErr_Format(PyExc_ValueError, "dt: %s is not on the current device", name);
+}
+/* the pointer of a contiguous tensor of `count` elements (at least, for a workspace's bytes), NULL for None */
+static void *whole(const dt_tensor_reader *rd, PyObject *t, const char *name, int kind, long long count, int device) {
+    static const char *const kinds[] = {"another type", "float32", "bfloat16", "int32", "uint8"};
+    dt_tensor_plain p;
+    if (t == Py_None) return NULL;
+    plain(rd, t, &p);
+    on_device(name, &p, device);
+    if (PyErr_Occurred()) return NULL;
+    if (p.kind != kind) PyErr_Format(PyExc_TypeError, "dt: %s is %s", name, kinds[kind]);
+    else if (!p.contiguous) PyErr_Format(PyExc_ValueError, "dt: %s is contiguous", name);
+    else if (p.numel != count) PyErr_Format(PyExc_ValueError, "dt: %s has %lld elements, got %lld", name, count, p.numel);
+    return ptr(rd, t);
+}
+/* rows of V elements side by side, float32 or bfloat16: pointer; *row = elements from one to the next */
+static void *rows_of(const dt_tensor_reader *rd, PyObject *t, const char *name, int device, long long *s, long long *row) {
+    dt_tensor_plain p;
+    shape(rd, t, 2, 1, s);
+    *row = stride(rd, t, 0);
+    if (s[0] == 1 && *row < s[1]) *row = s[1]; /* one row: its stride says nothing */
+    plain(rd, t, &p);
+    on_device(name, &p, device);
+    if (!PyErr_Occurred() && s[1] > 1 && stride(rd, t, 1) != 1) PyErr_Format(PyExc_ValueError, "dt: %s: the entries of a row lie side by side", name);
+    return ptr(rd, t);
 }
 
 #define NEED(n)                                                                                      \
@@ -298,6 +368,104 @@ FN(reward_step) {
     shape(rd, a[0], 1, 0, b);
     CALL(dt_reward_step(st, (int)b[0], len, bonus, secs, per, p[0], p[1], p[2], p[3], p[4]));
 }
+/* logits [B, rows, V], row_of, tokens [B, per_seq], temperature, k, logprob, entropy, stats [B, per_seq, 2], top_logprob,
+   top_id [B, per_seq, k], ws */
+FN(token_logprobs) {
+    NEED_TENSORS(11)
+    int dev;
+    void *const st = stream_on(&dev);
+    long long s[3], e[3], row = 0;
+    const int k = inum(a[4]);
+    const float temp = fnum(a[3]);
+    const dt_dtype t = dtype(rd, a[0]);
+    dt_tensor_plain p;
+    void *x, *o[5], *of, *tok, *w;
+    long long n;
+    shape(rd, a[0], 3, 1, s);
+    shape(rd, a[7], 3, 1, e);
+    n = e[0] * e[1];
+    plain(rd, a[0], &p);
+    on_device("logits", &p, dev);
+    if (!PyErr_Occurred()) {
+        row = s[1] > 1 ? stride(rd, a[0], 1) : s[0] > 1 ? stride(rd, a[0], 0) : s[2];
+        if (e[0] != s[0] || e[2] != 2) PyErr_Format(PyExc_ValueError, "dt: stats are [%lld, entries, 2]", s[0]);
+        else if ((s[2] > 1 && stride(rd, a[0], 2) != 1) || (s[0] > 1 && s[1] > 1 && stride(rd, a[0], 0) != s[1] * row))
+            PyErr_SetString(PyExc_ValueError, "dt: logits: the entries of a row lie side by side, the rows at one stride");
+        else if (e[1] > INT32_MAX || s[0] > INT32_MAX || s[2] > INT32_MAX) PyErr_SetString(PyExc_OverflowError, "argument does not fit an int");
+    }
+    x = ptr(rd, a[0]);
+    of = whole(rd, a[1], "row_of", DT_KIND_I32, n, dev);
+    tok = whole(rd, a[2], "tokens", DT_KIND_I32, n, dev);
+    o[0] = whole(rd, a[5], "logprob", DT_KIND_F32, n, dev);
+    o[1] = whole(rd, a[6], "entropy", DT_KIND_F32, n, dev);
+    o[2] = whole(rd, a[7], "stats", DT_KIND_F32, 2 * n, dev);
+    o[3] = k > 0 ? whole(rd, a[8], "top_logprob", DT_KIND_F32, n * k, dev) : NULL;
+    o[4] = k > 0 ? whole(rd, a[9], "top_id", DT_KIND_I32, n * k, dev) : NULL;
+    w = whole(rd, a[10], "ws", DT_KIND_U8, (long long)nbytes(rd, a[10]), dev);
+    const size_t wb = nbytes(rd, a[10]);
+    CALL(dt_token_logprobs(st, (int)s[0], (int)e[1], x, t, (int)s[2], row, s[1], of, tok, temp, k, o[0], o[1], o[2], o[3], o[4], w, wb));
+}
+static void same_rows(const long long *g, const long long *s, dt_dtype gt, dt_dtype t) {
+    if (PyErr_Occurred()) return;
+    if (g[0] != s[0] || g[1] != s[1]) PyErr_Format(PyExc_ValueError, "dt: grad is [%lld, %lld]", s[0], s[1]);
+    else if (gt != t) PyErr_SetString(PyExc_TypeError, "dt: grad has the logits' type");
+}
+/* logits [n, V], tokens, temperature, stats [n, 2], entropy, grad_logprob, grad_entropy, grad [n, V] */
+FN(token_logprobs_grad) {
+    NEED_TENSORS(8)
+    int dev;
+    void *const st = stream_on(&dev);
+    long long s[2], g[2], row, grow;
+    void *const x = rows_of(rd, a[0], "logits", dev, s, &row), *const gr = rows_of(rd, a[7], "grad", dev, g, &grow);
+    const dt_dtype t = dtype(rd, a[0]);
+    const float temp = fnum(a[2]);
+    void *const tok = whole(rd, a[1], "tokens", DT_KIND_I32, s[0], dev), *const stats = whole(rd, a[3], "stats", DT_KIND_F32, 2 * s[0], dev);
+    void *const h = whole(rd, a[4], "entropy", DT_KIND_F32, s[0], dev), *const gl = whole(rd, a[5], "grad_logprob", DT_KIND_F32, s[0], dev);
+    void *const gh = whole(rd, a[6], "grad_entropy", DT_KIND_F32, s[0], dev);
+    same_rows(g, s, dtype(rd, a[7]), t);
+    CALL(dt_token_logprobs_grad(st, s[0], x, t, (int)s[1], row, tok, temp, stats, h, gl, gh, gr, grow));
+}
+/* logits [n, V], teacher_val, teacher_id [m, k], teacher_lse [m], teacher_row [n], temperature, flags, grad_loss [n],
+   loss [n], stats [n, 2], tail [n], grad [n, V], ws;  without loss and ws: the gradient alone */
+static PyObject *distill(PyObject *const *a, Py_ssize_t nargs, const dt_tensor_reader *rd) {
+    const int both = nargs == 13;
+    PyObject *const *const b = a + (both ? 9 : 8); /* stats, tail, grad */
+    int dev;
+    void *const st = stream_on(&dev);
+    long long s[2], m[2], g[2] = {0, 0}, row, grow = 0;
+    void *const x = rows_of(rd, a[0], "logits", dev, s, &row);
+    const dt_dtype t = dtype(rd, a[0]);
+    void *val, *id, *lse, *of, *w, *loss, *stats, *tail, *grad = NULL, *ws;
+    const float temp = fnum(a[5]);
+    const int flags = inum(a[6]);
+    size_t wb;
+    shape(rd, a[1], 2, 1, m);
+    val = whole(rd, a[1], "teacher_val", DT_KIND_F32, m[0] * m[1], dev);
+    id = whole(rd, a[2], "teacher_id", DT_KIND_I32, m[0] * m[1], dev);
+    lse = whole(rd, a[3], "teacher_lse", DT_KIND_F32, m[0], dev);
+    of = whole(rd, a[4], "teacher_row", DT_KIND_I32, s[0], dev);
+    w = whole(rd, a[7], "grad_loss", DT_KIND_F32, s[0], dev);
+    loss = both ? whole(rd, a[8], "loss", DT_KIND_F32, s[0], dev) : NULL;
+    stats = whole(rd, b[0], "stats", DT_KIND_F32, 2 * s[0], dev);
+    tail = whole(rd, b[1], "tail", DT_KIND_F32, s[0], dev);
+    if (b[2] != Py_None) {
+        grad = rows_of(rd, b[2], "grad", dev, g, &grow);
+        same_rows(g, s, dtype(rd, b[2]), t);
+    }
+    if (!PyErr_Occurred() && m[1] > INT32_MAX) PyErr_SetString(PyExc_OverflowError, "argument does not fit an int");
+    if (!both) CALL(dt_distill_rows_grad(st, s[0], x, t, (int)s[1], row, (int)m[1], m[0], val, id, lse, of, temp, flags, w, stats, tail, grad, grow));
+    wb = nbytes(rd, a[12]);
+    ws = whole(rd, a[12], "ws", DT_KIND_U8, (long long)wb, dev);
+    CALL(dt_distill_rows(st, s[0], x, t, (int)s[1], row, (int)m[1], m[0], val, id, lse, of, temp, flags, w, loss, stats, tail, grad, grow, ws, wb));
+}
+FN(distill_rows) {
+    NEED_TENSORS(13)
+    return distill(a, nargs, rd);
+}
+FN(distill_rows_grad) {
+    NEED_TENSORS(11)
+    return distill(a, nargs, rd);
+}
 /* torch.float32, torch.bfloat16, callable -> current device, callable(device) -> its current raw stream */
 FN(setup) {
     NEED(4)
@@ -322,7 +490,8 @@ FN(set_reader) {
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {ENTRY(topk_rows), ENTRY(topk_rows_static), ENTRY(build_tree), ENTRY(tree_attention),
                                 ENTRY(accept_tree), ENTRY(expand_level), ENTRY(finish_tree), ENTRY(policy_step),
-                                ENTRY(commit), ENTRY(reward_step), ENTRY(setup), ENTRY(set_reader),
+                                ENTRY(commit), ENTRY(reward_step), ENTRY(token_logprobs), ENTRY(token_logprobs_grad),
+                                ENTRY(distill_rows), ENTRY(distill_rows_grad), ENTRY(setup), ENTRY(set_reader),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dtcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -332,6 +501,11 @@ PyMODINIT_FUNC PyInit__dtcall(void) {
     s_stride = PyUnicode_InternFromString("stride");
     s_dtype = PyUnicode_InternFromString("dtype");
     s_nbytes = PyUnicode_InternFromString("nbytes");
-    if (!s_data_ptr || !s_shape || !s_stride || !s_dtype || !s_nbytes) return NULL;
+    s_numel = PyUnicode_InternFromString("numel");
+    s_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_device = PyUnicode_InternFromString("device");
+    s_type = PyUnicode_InternFromString("type");
+    s_index = PyUnicode_InternFromString("index");
+    if (!s_data_ptr || !s_shape || !s_stride || !s_dtype || !s_nbytes || !s_numel || !s_contiguous || !s_device || !s_type || !s_index) return NULL;
     return PyModule_Create(&module);
 }

@@ -48,8 +48,18 @@ int dtype(PyObject *t, int *bf16) {
 int nbytes(PyObject *t, size_t *out) {
     return read(t, [&](const at::Tensor &x) { *out = x.nbytes(); return true; });
 }
+int plain(PyObject *t, dt_tensor_plain *out) {
+    return read(t, [&](const at::Tensor &x) {
+        const at::ScalarType s = x.scalar_type();
+        out->kind = s == at::kFloat ? DT_KIND_F32 : s == at::kBFloat16 ? DT_KIND_BF16 : s == at::kInt ? DT_KIND_I32 : s == at::kByte ? DT_KIND_U8 : DT_KIND_OTHER;
+        out->device = x.is_cuda() ? (int)x.get_device() : -1;
+        out->contiguous = x.is_contiguous();
+        out->numel = x.numel();
+        return true;
+    });
+}
 
-dt_tensor_reader table = {overridden, data_ptr, sizes, stride, dtype, nbytes};
+dt_tensor_reader table = {overridden, data_ptr, sizes, stride, dtype, nbytes, plain};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dttensor", NULL, -1, NULL, NULL, NULL, NULL, NULL};
 
 }  // namespace

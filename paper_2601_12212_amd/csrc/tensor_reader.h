@@ -10,6 +10,11 @@
 
 #define DT_TENSOR_READER "paper_2601_12212_amd.tensor_reader" /* the capsule's name */
 
+enum { DT_KIND_OTHER = 0, DT_KIND_F32, DT_KIND_BF16, DT_KIND_I32, DT_KIND_U8 };
+typedef struct {
+    int kind, device /* -1: not a GPU's */, contiguous;
+    long long numel;
+} dt_tensor_plain;
 typedef struct {
     int (*overridden)(void);
     int (*data_ptr)(PyObject *t, void **out);
@@ -17,5 +22,6 @@ typedef struct {
     int (*stride)(PyObject *t, long dim, long long *out);
     int (*dtype)(PyObject *t, int *bf16);                        /* float32 or bfloat16, no other */
     int (*nbytes)(PyObject *t, size_t *out);
+    int (*plain)(PyObject *t, dt_tensor_plain *out);
 } dt_tensor_reader;
 #endif

@@ -75,6 +75,7 @@ class Step:
         nbytes = B.dt_workspace_bytes(Bz, self.total_rows, V, TC, Hq, D)
         self.ws = torch.zeros(nbytes, dtype=torch.uint8, device=dev)
         self.scale = 1.0 / float(np.sqrt(D))
+        self._buffers = {}  # of token_logprobs and draft_loss, by what was asked for
 
     # ---- uploads (numpy float32 or bf16 bit patterns) ----------------------------------------
     def set_draft(self, b, rows):
@@ -121,6 +122,53 @@ class Step:
         self.build_tree()
         self.tree_attention()
         self.accept(philox_step)
+
+    # ---- what the step says of tokens, for its user and for the draft model's training -------------------
+    def token_logprobs(self, k=0):
+        """Log-probabilities of the tokens that the last accept() has emitted, each by the target's row that it was read from (out_tokens by
+        path_nodes; 0 behind the bonus token), at the temperature of the acceptance (greedy: 1), with the rows' entropies and k
+        alternatives.  -> dict of [B, DT_D_MAX + 1(, k)] tensors, overwritten by the next call with the same k."""
+        b = self._row_buffers(("emitted", k), self.out_tokens.shape[1], k)
+        B.dt_token_logprobs(self.target_logits, self.path_nodes, self.out_tokens,
+                            1.0 if self.mode == B.DT_ACCEPT_GREEDY else self.temperature, k, b["logprob"], b["entropy"], b["stats"],
+                            b["top_logprob"], b["top_id"], b["ws"])
+        return b
+
+    def draft_loss(self, k=20, flags=B.DT_DISTILL_TAIL, temperature=1.0, grad_loss=None, grad=None):
+        """The distillation loss of the draft rows against the target rows of the nodes that they were handed to (src_row): the
+        pairs of the two models' answers to the same tokens that a step leaves behind.  Rows that belong to no node of the tree have loss 0.  grad
+        [total_rows, V], if given, takes the gradient in draft_logits, weighted by grad_loss [total_rows].
+        -> loss [total_rows], overwritten by the next call with the same k."""
+        Bz, TC, dev = self.Bsz, self.TT_cap, self.device
+        node = torch.arange(TC, dtype=torch.int32, device=dev).expand(Bz, TC)
+        live = node < self.n_nodes[:, None]
+        t = self._row_buffers(("nodes", k), TC, k)
+        B.dt_token_logprobs(self.target_logits, torch.where(live, node, -1), None, temperature, k, None, None, t["stats"], t["top_logprob"],
+                            t["top_id"], t["ws"])
+        # which node every draft row was handed to: rows of nodes that were not expanded go to a place behind the last
+        row = torch.where(live & (self.src_row >= 0), self.row_off[:Bz, None] + self.src_row, self.total_rows)
+        of = torch.full((self.total_rows + 1,), -1, dtype=torch.int32, device=dev)
+        of.scatter_(0, row.reshape(-1), torch.arange(Bz * TC, dtype=torch.int32, device=dev))
+        d = self._buffers.get(("draft", k))
+        if d is None:
+            f32 = dict(dtype=torch.float32, device=dev)
+            ws = torch.empty(B.dt_logprob_workspace_bytes(self.total_rows, self.V), dtype=torch.uint8, device=dev)
+            d = self._buffers[("draft", k)] = dict(loss=torch.empty(self.total_rows, **f32), stats=torch.empty((self.total_rows, 2), **f32),
+                                                   tail=torch.empty(self.total_rows, **f32), ws=ws)
+        B.dt_distill_rows(self.draft_logits, t["top_logprob"].view(Bz * TC, k), t["top_id"].view(Bz * TC, k), None, of[:-1], temperature, flags,
+                          grad_loss, d["loss"], d["stats"], d["tail"], grad, d["ws"])
+        return d["loss"]
+
+    def _row_buffers(self, key, n, k):
+        b = self._buffers.get(key)
+        if b is None:
+            f32 = dict(dtype=torch.float32, device=self.device)
+            b = self._buffers[key] = dict(
+                logprob=torch.empty((self.Bsz, n), **f32), entropy=torch.empty((self.Bsz, n), **f32),
+                stats=torch.empty((self.Bsz, n, 2), **f32), top_logprob=torch.empty((self.Bsz, n, k), **f32) if k else None,
+                top_id=torch.empty((self.Bsz, n, k), dtype=torch.int32, device=self.device) if k else None,
+                ws=torch.empty(B.dt_logprob_workspace_bytes(self.Bsz * n, self.V), dtype=torch.uint8, device=self.device))
+        return b
 
     # ---- the same three calls with the argument lists marshalled once ---------------------------
     def prepare(self):
