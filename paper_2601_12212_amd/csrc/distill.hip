@@ -7,167 +7,196 @@
 //     d / dx_j = w / T [ (P + p_t) q_j - (j outside S: p_t q_j / q_t) - (sum of p_i with id_i = j) ]
 // Both sides of q_t come from sums of their own, S's elements left out of the stream and added one by one: 1 - (sum in S) would have no digits
 // left where the student is sure.  Outside S every gradient is q_j times one factor of the row, for log-probabilities and entropies q_j times a linear
-// function of log q_j: one exponential an element, read and written once, and the few elements of S are written over at the end.
+// function of log q_j: one exponential an element, which is read and written once by one thread, so that a gradient may take its logits' place.
+//
+// Which elements belong to S a wave knows from its lanes: lane i holds where entries i and 64 + i lie (go, thread, element of the thread), a ballot
+// at every go finds those of the wave's own, rarely one.
 #include "vocab_rows.hpp"
 
 namespace dt {
 
 // ---- the teacher's entries for a row ----
-struct Teacher {
-    int id[DT_DISTILL_K_MAX];    // -1: none
-    float p[DT_DISTILL_K_MAX], lp[DT_DISTILL_K_MAX];
-    float sum[DT_DISTILL_K_MAX]; // p of all entries with this id, in the first of them; -1 in the others
-    double part[VR_NT / 64];
-    float P, rest;
-    Sums in_s;                   // the student's elements of S
-    float loss;
+#define SLOTS (DT_DISTILL_K_MAX / 64)  // entries of a lane
+struct Teacher {                       // the entries, as the first wave leaves them for all
+    double p[DT_DISTILL_K_MAX], lp[DT_DISTILL_K_MAX];
+    float sum[DT_DISTILL_K_MAX];       // p of all entries with the same id
+    float x[DT_DISTILL_K_MAX];         // the student's logits
+    int id[DT_DISTILL_K_MAX];          // -1: none
+    float P, rest, in_m, in_s;         // the student's sum in S
+};
+struct Entries {  // of a lane: where they are worked on
+    int where[SLOTS];   // go * waves + wave, -1: a loose element, -2: none
+    int which[SLOTS];   // lane | element << 6
+};
+struct Given {  // as they were given
+    int id[SLOTS];
+    float val[SLOTS];
 };
 // The teacher's row, -1: none.
 __device__ __forceinline__ int64_t teacher_row(const DistillArgs &a, int64_t r) {
     const int64_t t = a.teacher_row ? (int64_t)a.teacher_row[r] : r;
     return t < 0 || t >= a.n_teacher ? -1 : t;
 }
+__device__ __forceinline__ void entries_load(const DistillArgs &a, int64_t tr, Given &G) {
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int i = 64 * s + lane_id();
+        G.id[s] = -1;
+        G.val[s] = -INFINITY;
+        if (i < a.k) {
+            G.id[s] = a.teacher_id[tr * a.k + i];
+            G.val[s] = a.teacher_val[tr * a.k + i];
+        }
+    }
+}
+template <int NT, int U, bool BF16>
+__device__ __forceinline__ void entries_place(const DistillArgs &a, const Row<BF16> &row, Given &G, Entries &E) {
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        if (!(G.id[s] >= 0 && G.id[s] < a.V && G.val[s] > -INFINITY)) G.id[s] = -1;
+        const Place p = place_of<BF16, NT, U>(row, max(G.id[s], 0));
+        E.where[s] = G.id[s] < 0 ? -2 : p.go < 0 ? -1 : p.go * (NT / 64) + (p.thread >> 6);
+        E.which[s] = (p.thread & 63) | p.elem << 6;
+    }
+}
+// f(lane, element, entry) for the entries at `where` (uniform): one after the other, the same for all lanes
+template <class F>
+__device__ __forceinline__ void entries_at(const DistillArgs &a, const Entries &E, int where, F f) {
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        if (s && a.k <= 64 * s) break;  // uniform
+        for (u64 b = ballot(E.where[s] == where); b; b &= b - 1) {
+            const int i = __builtin_ctzll(b), w = __builtin_amdgcn_readlane(E.which[s], i);
+            f(w & 63, w >> 6, 64 * s + i);
+        }
+    }
+}
+// what lanes of a wave have left in shared memory, for its other lanes
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) v += __hiloint2double(__shfl_xor(__double2hiint(v), o, 64), __shfl_xor(__double2loint(v), o, 64));
     return v;
 }
-__device__ __forceinline__ double block_sum_f64(double v, double (&room)[VR_NT / 64]) {
-    v = wave_sum_f64(v);
-    __syncthreads();
-    if (lane_id() == 0) room[threadIdx.x >> 6] = v;
-    __syncthreads();
-    double r = room[0];
+// By one wave: the entries into `t`; x: the student's logits.  Probabilities in 64 bits, since 1 - P is one of them.
+__device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, const Given &G, const float (&x)[SLOTS], Teacher &t) {
+    const int lane = lane_id();
+    double P = 0.0, p[SLOTS], lp[SLOTS];
 #pragma unroll
-    for (int i = 1; i < VR_NT / 64; ++i) r += room[i];
-    return r;
-}
-// Probabilities in 64 bits, since 1 - P is one of them.  Ends with a barrier.
-__device__ __forceinline__ void teacher_load(const DistillArgs &a, int64_t tr, Teacher &t) {
-    const int tid = threadIdx.x;
-    double lp = 0.0, p = 0.0;
-    if (tid < a.k) {
-        const int id = a.teacher_id[tr * a.k + tid];
-        const float val = a.teacher_val[tr * a.k + tid], lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f;
-        const bool there = id >= 0 && id < a.V && val > -INFINITY;
-        if (there) {
-            lp = (double)val - (double)lse;
-            p = exp(lp);
+    for (int s = 0; s < SLOTS; ++s) {
+        p[s] = lp[s] = 0.0;
+        if (G.id[s] >= 0) {
+            lp[s] = (double)G.val[s] - (double)lse;
+            p[s] = exp(lp[s]);
+            P += p[s];
         }
-        t.id[tid] = there ? id : -1;
     }
-    double P = block_sum_f64(p, t.part);
+    P = wave_sum_f64(P);
     if ((a.flags & DT_DISTILL_RENORM) && P > 0.0) {
-        p /= P;
-        lp -= log(P);
+        const double l = log(P);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            p[s] /= P;
+            lp[s] -= l;
+        }
         P = 1.0;
     }
-    if (tid < a.k) {
-        t.p[tid] = (float)p;
-        t.lp[tid] = (float)lp;
-    }
-    if (tid == 0) {
-        t.rest = (a.flags & DT_DISTILL_TAIL) ? (float)fmax(0.0, 1.0 - P) : 0.f;
-        t.P = (float)P;
-    }
-    __syncthreads();
-    if (tid < a.k) {
-        const int id = t.id[tid];
-        float sum = 0.f;
-        bool first = id >= 0;
-        for (int j = 0; j < a.k; ++j)
-            if (t.id[j] == id) {
-                sum += t.p[j];
-                first &= j >= tid;
-            }
-        t.sum[tid] = first ? sum : -1.f;
-    }
-    __syncthreads();
-}
-
-// ---- elements of S in a stretch: a bit for each of a thread's 32 elements of a go, and one for each loose one ----
-__device__ __forceinline__ void marks_clear(u32 *marks, int goes) {
-    for (int i = threadIdx.x; i <= goes * VR_NT; i += VR_NT) marks[i] = 0;
-}
-template <bool BF16>
-__device__ __forceinline__ void mark(const Stretch<BF16> &st, u32 *marks, int at) {  // at: place in the stretch
-    const int u8 = at - st.head;
-    if (u8 < 0 || u8 >= 8 * st.units) {
-        const int i = u8 < 0 ? at : at - 8 * st.units;
-        atomicOr(&marks[st.goes() * VR_NT], 1u << i);
-        return;
-    }
-    const int unit = u8 >> 3, it = unit / VR_GO, u = unit % VR_GO / VR_NT, t = unit % VR_NT;
-    atomicOr(&marks[it * VR_NT + t], 1u << (8 * u + (u8 & 7)));
-}
-
-// The sums of a stretch without the elements of S.
-template <bool BF16, bool KEEP>
-__device__ __forceinline__ Sums sums_outside(const Stretch<BF16> &st, const u32 *marks, float c) {
-    Sums r = {-INFINITY, 0.f, 0.f};
-    const int goes = st.goes();
-    for (int it = 0; it < goes; ++it) {
-        Raw<BF16> raw;
-        go_request<BF16, KEEP>(st, it, raw);
-        float x[8 * VR_U];
-        go_finish<BF16>(st, it, raw, x);
-        const u32 m = marks[it * VR_NT + threadIdx.x];
-        if (m) {
+    // sums over entries with the same id, mostly one
+    bool first[SLOTS], twice = false;
 #pragma unroll
-            for (int j = 0; j < 8 * VR_U; ++j) x[j] = m >> j & 1 ? -INFINITY : x[j];
-        }
-        sums_add<false>(r, x, max_of(x), c);
+    for (int s = 0; s < SLOTS; ++s) {
+        t.id[64 * s + lane] = G.id[s];
+        t.p[64 * s + lane] = p[s];
+        t.lp[64 * s + lane] = lp[s];
+        t.sum[64 * s + lane] = (float)p[s];
+        t.x[64 * s + lane] = x[s];
+        first[s] = G.id[s] >= 0;
     }
-    if ((int)threadIdx.x < st.loose && !(marks[goes * VR_NT] >> threadIdx.x & 1))
-        sums_add1<false>(r, Elem<BF16>::get(st.p + st.loose_at(threadIdx.x)), c);
-    return r;
+    wave_sync();
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        if (s && a.k <= 64 * s) break;
+        int same = 0;
+        for (int j = 0; j < a.k; ++j) same += t.id[j] == G.id[s];
+        twice |= G.id[s] >= 0 && same > 1;
+    }
+    if (ballot(twice)) {
+        float sum[SLOTS];
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            sum[s] = 0.f;
+            for (int j = 0; j < a.k; ++j)
+                if (t.id[j] == G.id[s]) {
+                    sum[s] += t.sum[j];
+                    first[s] = first[s] && j >= 64 * s + lane;
+                }
+        }
+        wave_sync();
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) t.sum[64 * s + lane] = sum[s];
+    }
+    // the student's elements of S, one for each id
+    Sums in = {-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+        if (first[s]) sums_add1<false>(in, x[s], a.c);
+    wave_sums<false>(in, a.c);
+    if (lane == 0) {
+        t.P = (float)P;
+        t.rest = (a.flags & DT_DISTILL_TAIL) ? (float)fmax(0.0, 1.0 - P) : 0.f;
+        t.in_m = in.m;
+        t.in_s = in.s;
+    }
 }
 
-// What both passes over a row go by.
+// ---- the loss ----
+// What the second pass over a row goes by.
 struct RowLoss {
     RowStat st;
     float tail;       // log of the probability outside S
     float in_s, out;  // factors of q_j in S and outside, w / T in them
 };
-// out: the row's sums outside S; x: thread tid's element of S, if it is the first of its id.  Writes loss, stats and tail where `tell`.
-__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, int64_t r, Teacher &t, Sums outside, float x, Sums (&room)[VR_NT / 64], bool tell) {
-    const int tid = threadIdx.x;
-    const bool mine = tid < a.k && t.id[tid] >= 0, first = mine && t.sum[tid] >= 0.f;
-    Sums s = {first ? x : -INFINITY, first && x > -INFINITY ? 1.f : 0.f, 0.f};
-    s = block_sums<false>(s, a.c, room);
-    const float m = fmaxf(s.m, outside.m);
-    sums_move<false>(s, m, a.c);
-    sums_move<false>(outside, m, a.c);
-    const float whole = s.s + outside.s;
+// from the row's sums in S and outside, by any thread
+__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, float w, const Teacher &t, Sums out) {
+    Sums in = {t.in_m, t.in_s, 0.f};
+    const float m = fmaxf(in.m, out.m);
+    sums_move<false>(in, m, a.c);
+    sums_move<false>(out, m, a.c);
+    const float whole = in.s + out.s;
     RowLoss R;
     R.st = row_stat(m, whole, a.c);
-    R.tail = !(whole > 0.f) ? -INFINITY : s.s < outside.s ? log1pf(-s.s / whole) : logf(outside.s / whole);
-    const float w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
+    R.tail = !(whole > 0.f) ? -INFINITY : in.s < out.s ? log1pf(-in.s / whole) : logf(out.s / whole);
     R.in_s = w * (t.P + t.rest);
-    R.out = outside.s > 0.f ? R.in_s - w * t.rest * (whole / outside.s) : R.in_s;
-    if (tell) {
-        double term = 0.0;
-        if (mine && t.p[tid] > 0.f) term = (double)t.p[tid] * ((double)t.lp[tid] - (double)log_prob(x, R.st, a.c));
-        if (tid == 0 && t.rest > 0.f) term += (double)t.rest * ((double)logf(t.rest) - (double)R.tail);
-        const double loss = block_sum_f64(term, t.part);
-        if (tid == 0) {
-            a.loss[r] = (float)loss;
-            a.stats[2 * r] = R.st.m;
-            a.stats[2 * r + 1] = R.st.l;
-            a.tail[r] = R.tail;
-        }
-    }
+    R.out = out.s > 0.f ? R.in_s - w * t.rest * (whole / out.s) : R.in_s;
     return R;
+}
+// by the first wave
+__device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, const Teacher &t, const RowLoss &R) {
+    double term = 0.0;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int i = 64 * s + lane_id();
+        const double p = t.p[i];
+        if (p > 0.0) term += p * (t.lp[i] - (double)log_prob(t.x[i], R.st, a.c));
+    }
+    if (lane_id() == 0 && t.rest > 0.f) term += (double)t.rest * ((double)logf(t.rest) - (double)R.tail);
+    term = wave_sum_f64(term);
+    if (lane_id() == 0) {
+        a.loss[r] = (float)term;
+        a.stats[2 * r] = R.st.m;
+        a.stats[2 * r + 1] = R.st.l;
+        a.tail[r] = R.tail;
+    }
 }
 __device__ __forceinline__ void row_loss_none(const DistillArgs &a, int64_t r) {
     if (threadIdx.x == 0) a.loss[r] = a.stats[2 * r] = a.stats[2 * r + 1] = a.tail[r] = 0.f;
 }
 
 // ---- gradients ----
-template <bool BF16>
-struct Out8 {
-    Vec16 r[BF16 ? 1 : 2];
-};
 __device__ __forceinline__ u32 to_bf16(float v) {  // to the nearest, ties to even: the one rounding of a gradient
     const u32 u = __float_as_uint(v);
     return (v != v ? 0x7FC00000u : u + 0x7FFFu + (u >> 16 & 1u)) >> 16;
@@ -209,222 +238,367 @@ __device__ __forceinline__ Slope slope(float m, float l, float c, float a, float
     // (nothing finite in the row: every q is 0)
     return m == -INFINITY ? Slope{0.f, INFINITY, c, a, b} : Slope{m, l * LOG2E, c, a, b};
 }
-template <bool BF16, bool ENT>
-__device__ __forceinline__ void grad_stretch(const Stretch<BF16> &st, const Slope &k, void *grad, int64_t at) {
-    const int goes = st.goes();
-    for (int it = 0; it < goes; ++it) {
-        Raw<BF16> raw;
-        go_request<BF16, false>(st, it, raw);
-        float x[8 * VR_U];
-        go_finish<BF16>(st, it, raw, x);
+// the gradients of a go, stored; at: where the row's gradient starts
+template <int NT, bool ENT, bool BF16, int N>
+__device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope &k, void *grad, int64_t at, const float (&x)[N]) {
 #pragma unroll
-        for (int u = 0; u < VR_U; ++u) {
-            const int unit = it * VR_GO + u * VR_NT + (int)threadIdx.x;
-            float g[8];
+    for (int u = 0; u < N / 8; ++u) {
+        const int unit = (it * (N / 8) + u) * NT + (int)threadIdx.x;
+        float g[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[8 * u + e]);
-            if (unit < st.units) put_unit<BF16>(grad, at + st.head + 8 * (int64_t)unit, g);
-        }
-    }
-    if ((int)threadIdx.x < st.loose) {
-        const int i = st.loose_at(threadIdx.x);
-        put_elem<BF16>(grad, at + i, slope_at<ENT>(k, Elem<BF16>::get(st.p + i)));
+        for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[8 * u + e]);
+        if (unit < row.units) put_unit<BF16>(grad, at + row.head + 8 * (int64_t)unit, g);
     }
 }
 template <bool BF16>
-__device__ __forceinline__ void grad_zero(void *grad, int64_t at, int n) {
-    for (int i = threadIdx.x; i < n; i += VR_NT) put_elem<BF16>(grad, at + i, 0.f);
+__device__ __forceinline__ void grad_zero(void *grad, int64_t at, int n, int nt) {
+    for (int i = threadIdx.x; i < n; i += nt) put_elem<BF16>(grad, at + i, 0.f);
+}
+// What the gradients of a row with a teacher go by.
+struct DistillSlope {
+    Slope out;
+    float in_s, w;
+    int64_t at;
+};
+// of a go: all as if outside S, then, by the same thread, those in S
+template <int NT, bool BF16, int N>
+__device__ __forceinline__ void distill_grad_go(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
+                                                const float (&x)[N]) {
+    put_go<NT, false>(row, it, d.out, a.grad, d.at, x);
+    Slope in = d.out;
+    in.a = d.in_s;
+    entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int, int i) {
+        const float g = slope_at<false>(in, t.x[i]) - d.w * t.sum[i];
+        if (lane_id() == lane) put_elem<BF16>(a.grad, d.at + t.id[i], g);
+    });
+}
+template <bool BF16>
+__device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, float x) {
+    if (row.loose == 0 || threadIdx.x >= 64) return;
+    float g = slope_at<false>(d.out, x);
+    Slope in = d.out;
+    in.a = d.in_s;
+    entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(in, x) - d.w * t.sum[i] : g; });
+    if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
+}
+// v(entry) in the place of the go's elements of S
+template <int NT, int N, class V>
+__device__ __forceinline__ void replace(const DistillArgs &a, const Entries &E, int it, float (&x)[N], V v) {
+    entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int elem, int i) {
+        const float y = v(i);
+        const bool mine = lane_id() == lane;
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = mine && j == elem ? y : x[j];
+    });
+}
+__device__ __forceinline__ float hide_loose(const DistillArgs &a, const Entries &E, float x) {
+    if (threadIdx.x >= 64) return x;
+    entries_at(a, E, -1, [&](int lane, int, int) { x = lane_id() == lane ? -INFINITY : x; });
+    return x;
+}
+template <bool BF16>
+__device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, float (&x)[SLOTS]) {
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) x[s] = G.id[s] >= 0 ? row.at(G.id[s]) : -INFINITY;
 }
 
-extern __shared__ __align__(16) u32 distill_marks[];
-
-template <bool BF16>
-__device__ __forceinline__ float elem_of(const void *logits, int64_t at) {
-    return Elem<BF16>::get((const typename Elem<BF16>::T *)logits + at);
-}
-// thread tid's element of S
-template <bool BF16>
-__device__ __forceinline__ float s_elem(const DistillArgs &a, int64_t row, const Teacher &t) {
-    const int tid = threadIdx.x;
-    return tid < a.k && t.id[tid] >= 0 ? elem_of<BF16>(a.logits, row + t.id[tid]) : -INFINITY;
-}
-// the gradients of S's elements in [id0, id0 + n), behind the stretch's
-template <bool BF16>
-__device__ __forceinline__ void grad_of_s(const DistillArgs &a, int64_t r, const Teacher &t, const Slope &in_s, float x, int id0, int n) {
-    const int tid = threadIdx.x;
-    __syncthreads();
-    if (tid < a.k && t.id[tid] >= id0 && t.id[tid] < id0 + n && t.sum[tid] >= 0.f) {
-        const float w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
-        put_elem<BF16>(a.grad, r * a.grad_stride + t.id[tid], slope_at<false>(in_s, x) - w * t.sum[tid]);
-    }
-}
-
-// Loss of whole rows, one to a workgroup, and their gradient in a second pass over the row, which the caches then hold.
-template <bool BF16, bool GRAD>
-__global__ __launch_bounds__(VR_NT) void distill_row_kernel(DistillArgs a) {
+// ---- rows that a workgroup holds: read once ----
+template <bool BF16, bool GRAD, int NT>
+__global__ __launch_bounds__(NT, 8) void distill_held_kernel(DistillArgs a) {
+    constexpr int U = 4;
     __shared__ Teacher t;
-    __shared__ Sums room[VR_NT / 64];
-    const int64_t r = blockIdx.x, row = r * a.row_stride;
+    __shared__ Sums room[NT / 64];
+    const int64_t r = blockIdx.x;
     const int64_t tr = teacher_row(a, r);
     if (tr < 0) {
         row_loss_none(a, r);
-        if (GRAD) grad_zero<BF16>(a.grad, r * a.grad_stride, a.V);
+        if (GRAD) grad_zero<BF16>(a.grad, r * a.grad_stride, a.V, NT);
         return;
     }
-    const Stretch<BF16> st(a.logits, row, a.V);
-    marks_clear(distill_marks, st.goes());
-    teacher_load(a, tr, t);
-    const float x = s_elem<BF16>(a, row, t);
-    if ((int)threadIdx.x < a.k && t.id[threadIdx.x] >= 0) mark<BF16>(st, distill_marks, t.id[threadIdx.x]);
-    __syncthreads();
-    Sums s = sums_outside<BF16, GRAD>(st, distill_marks, a.c);
-    s = block_sums<false>(s, a.c, room);
-    const RowLoss R = row_loss(a, r, t, s, x, room, true);
+    const bool lead = threadIdx.x < 64;
+    const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
+    const Row<BF16> row(a.logits, r * a.row_stride, a.V);
+    Given G;
+    entries_load(a, tr, G);
+    Raw<BF16, U> raw;
+    if (row.units > 0) go_request<NT, false>(row, 0, raw);
+    const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
+    Entries E;
+    entries_place<NT, U>(a, row, G, E);
+    if (lead) {
+        float xs[SLOTS];
+        s_elems<BF16>(row, G, xs);
+        teacher_probs(a, lse, G, xs, t);
+    }
+    float x[8 * U];
+    go_finish<NT>(row, 0, raw, x);
+    replace<NT>(a, E, 0, x, [](int) { return -INFINITY; });
+    Sums s = {-INFINITY, 0.f, 0.f};
+    sums_add<false>(s, x, max_of(x), a.c);
+    if (row.loose > 0) sums_add1<false>(s, hide_loose(a, E, xl), a.c);
+    s = block_sums<false, NT>(s, a.c, room);
+    const RowLoss R = row_loss(a, w, t, s);
+    if (lead) loss_write(a, r, t, R);
     if (GRAD) {
-        grad_stretch<BF16, false>(st, slope(R.st.m, R.st.l, a.c, R.out, 0.f), a.grad, r * a.grad_stride);
-        grad_of_s<BF16>(a, r, t, slope(R.st.m, R.st.l, a.c, R.in_s, 0.f), x, 0, a.V);
+        const DistillSlope d = {slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride};
+        replace<NT>(a, E, 0, x, [&](int i) { return t.x[i]; });
+        distill_grad_go<NT>(a, row, 0, E, t, d, x);
+        distill_grad_loose(a, row, E, t, d, xl);
     }
 }
 
-// Sums outside S of a part of a row, and the elements of S in it (the next launch may write their gradients over them).
+// ---- rows that are streamed ----
+// A workgroup's sums outside S over goes first .. end - 1, and the loose elements where `loose`.
+template <bool BF16, bool KEEP>
+__device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF16> &row, const Entries &E, int first, int end, bool loose) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    Sums s = {-INFINITY, 0.f, 0.f};
+    for (int it = first; it < end; ++it) {
+        Raw<BF16, U> raw;
+        go_request<NT, KEEP>(row, it, raw);
+        float x[8 * U];
+        go_finish<NT>(row, it, raw, x);
+        replace<NT>(a, E, it, x, [](int) { return -INFINITY; });
+        sums_add<false>(s, x, max_of(x), a.c);
+    }
+    if (loose && row.loose > 0) {
+        const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
+        sums_add1<false>(s, hide_loose(a, E, xl), a.c);
+    }
+    return s;
+}
 template <bool BF16>
-__global__ __launch_bounds__(VR_NT) void distill_part_kernel(DistillArgs a) {
-    __shared__ Sums room[VR_NT / 64];
-    const int64_t r = blockIdx.x, row = r * a.row_stride;
-    const int part = blockIdx.y, tid = threadIdx.x, id0 = part * a.part_elems, n = min(a.V - id0, a.part_elems);
+__device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, int first, int end,
+                                          bool loose) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    for (int it = first; it < end; ++it) {
+        Raw<BF16, U> raw;
+        go_request<NT, false>(row, it, raw);
+        float x[8 * U];
+        go_finish<NT>(row, it, raw, x);
+        distill_grad_go<NT>(a, row, it, E, t, d, x);
+    }
+    if (loose) {
+        const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
+        distill_grad_loose(a, row, E, t, d, xl);
+    }
+}
+
+// Whole rows, and their gradient in a second pass over the row, which the caches then hold.
+template <bool BF16, bool GRAD>
+__global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    __shared__ Teacher t;
+    __shared__ Sums room[NT / 64];
+    const int64_t r = blockIdx.x;
+    const int64_t tr = teacher_row(a, r);
+    if (tr < 0) {
+        row_loss_none(a, r);
+        if (GRAD) grad_zero<BF16>(a.grad, r * a.grad_stride, a.V, NT);
+        return;
+    }
+    const bool lead = threadIdx.x < 64;
+    const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
+    const Row<BF16> row(a.logits, r * a.row_stride, a.V);
+    const int goes = row.template goes<STREAM_GO>();
+    Given G;
+    Entries E;
+    entries_load(a, tr, G);
+    entries_place<NT, U>(a, row, G, E);
+    if (lead) {
+        float xs[SLOTS];
+        s_elems<BF16>(row, G, xs);
+        teacher_probs(a, lse, G, xs, t);
+    }
+    Sums s = sums_outside<BF16, GRAD>(a, row, E, 0, goes, true);
+    s = block_sums<false, NT>(s, a.c, room);
+    const RowLoss R = row_loss(a, w, t, s);
+    if (lead) loss_write(a, r, t, R);
+    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true);
+}
+
+// Sums outside S of a part of a row, and from the first part the elements of S (the next launch may write their gradients over them).
+template <bool BF16>
+__global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    __shared__ Sums room[NT / 64];
+    const int64_t r = blockIdx.x;
+    const int part = blockIdx.y, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
     if (tr < 0) return;
-    const Stretch<BF16> st(a.logits, row + id0, n);
-    marks_clear(distill_marks, st.goes());
-    __syncthreads();
-    if (tid < a.k) {
-        const int id = a.teacher_id[tr * a.k + tid];
-        if (id >= id0 && id < id0 + n && a.teacher_val[tr * a.k + tid] > -INFINITY) {
-            mark<BF16>(st, distill_marks, id - id0);
-            a.s_elems[r * a.k + tid] = elem_of<BF16>(a.logits, row + id);
-        }
+    const Row<BF16> row(a.logits, r * a.row_stride, a.V);
+    Given G;
+    Entries E;
+    entries_load(a, tr, G);
+    entries_place<NT, U>(a, row, G, E);
+    if (part == 0 && threadIdx.x < 64) {
+        float xs[SLOTS];
+        s_elems<BF16>(row, G, xs);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (64 * s + lane_id() < a.k) a.s_elems[r * a.k + 64 * s + lane_id()] = xs[s];
     }
-    __syncthreads();
-    Sums s = sums_outside<BF16, true>(st, distill_marks, a.c);
-    s = block_sums<false>(s, a.c, room);
-    if (tid == 0) ((float2 *)a.ws)[r * a.parts + part] = make_float2(s.m, s.s);
-}
-// the parts of a row (up to 64) together, in every thread
-__device__ __forceinline__ Sums join_parts(const DistillArgs &a, int64_t r) {
-    Sums s = {-INFINITY, 0.f, 0.f};
-    if (lane_id() < a.parts) {
-        const float2 p = ((const float2 *)a.ws)[r * a.parts + lane_id()];
-        s.m = p.x;
-        s.s = p.y;
-    }
-    sums_move<false>(s, wave_max(s.m), a.c);
-    s.s = wave_sum(s.s);
-    return s;
+    Sums s = sums_outside<BF16, true>(a, row, E, first, min(first + a.part_goes, row.template goes<STREAM_GO>()), part == 0);
+    s = block_sums<false, NT>(s, a.c, room);
+    if (threadIdx.x == 0) ((float2 *)a.ws)[r * a.parts + part] = make_float2(s.m, s.s);
 }
 // The loss of rows whose parts are there, and with GRAD the gradient of a part.
 template <bool BF16, bool GRAD>
-__global__ __launch_bounds__(VR_NT) void distill_join_kernel(DistillArgs a) {
+__global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
-    __shared__ Sums room[VR_NT / 64];
-    const int64_t r = blockIdx.x, row = r * a.row_stride;
-    const int part = blockIdx.y, id0 = part * a.part_elems, n = GRAD ? min(a.V - id0, a.part_elems) : 0;
+    const int64_t r = blockIdx.x;
+    const int part = blockIdx.y, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
+    const Row<BF16> row(a.logits, r * a.row_stride, a.V);
+    const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
     if (tr < 0) {
         if (part == 0) row_loss_none(a, r);
-        if (GRAD) grad_zero<BF16>(a.grad, r * a.grad_stride + id0, n);
+        const int from = min(part * a.part_goes * STREAM_ELEMS, a.V), to = min((part + 1) * a.part_goes * STREAM_ELEMS, a.V);
+        if (GRAD) grad_zero<BF16>(a.grad, r * a.grad_stride + from, to - from, NT);
         return;
     }
-    teacher_load(a, tr, t);
-    const float x = (int)threadIdx.x < a.k && t.id[threadIdx.x] >= 0 ? a.s_elems[r * a.k + threadIdx.x] : -INFINITY;
-    const RowLoss R = row_loss(a, r, t, join_parts(a, r), x, room, part == 0);
-    if (GRAD) {
-        const Stretch<BF16> st(a.logits, row + id0, n);
-        grad_stretch<BF16, false>(st, slope(R.st.m, R.st.l, a.c, R.out, 0.f), a.grad, r * a.grad_stride + id0);
-        grad_of_s<BF16>(a, r, t, slope(R.st.m, R.st.l, a.c, R.in_s, 0.f), x, id0, n);
+    const bool lead = threadIdx.x < 64;
+    if (!GRAD && !lead) return;
+    const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
+    Sums out = {-INFINITY, 0.f, 0.f};
+    if (lane_id() < a.parts) {
+        const float2 p = ((const float2 *)a.ws)[r * a.parts + lane_id()];
+        out.m = p.x;
+        out.s = p.y;
     }
+    Given G;
+    Entries E;
+    entries_load(a, tr, G);
+    entries_place<NT, U>(a, row, G, E);
+    wave_sums<false>(out, a.c);
+    if (lead) {
+        float xs[SLOTS];
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) xs[s] = G.id[s] >= 0 ? a.s_elems[r * a.k + 64 * s + lane_id()] : -INFINITY;
+        teacher_probs(a, lse, G, xs, t);
+    }
+    if (GRAD) __syncthreads();
+    else wave_sync();
+    const RowLoss R = row_loss(a, w, t, out);
+    if (lead && part == 0) loss_write(a, r, t, R);
+    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0);
 }
 
 // The gradient of a part of a row from what the loss has saved.
 template <bool BF16>
-__global__ __launch_bounds__(VR_NT) void distill_grad_kernel(DistillArgs a) {
+__global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
-    const int64_t r = blockIdx.x, row = r * a.row_stride;
-    const int id0 = blockIdx.y * a.part_elems, n = min(a.V - id0, a.part_elems);
+    const int64_t r = blockIdx.x;
+    const int part = blockIdx.y, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
+    const Row<BF16> row(a.logits, r * a.row_stride, a.V);
     if (tr < 0) {
-        grad_zero<BF16>(a.grad, r * a.grad_stride + id0, n);
+        const int from = min(part * a.part_goes * STREAM_ELEMS, a.V), to = min((part + 1) * a.part_goes * STREAM_ELEMS, a.V);
+        grad_zero<BF16>(a.grad, r * a.grad_stride + from, to - from, NT);
         return;
     }
+    const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const float m = a.stats[2 * r], l = a.stats[2 * r + 1], tail = a.tail[r];
-    teacher_load(a, tr, t);
-    const float x = s_elem<BF16>(a, row, t);
-    const float w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t, in_s = w * (t.P + t.rest);
-    const float out = tail > -INFINITY ? in_s - w * t.rest * expf(-tail) : in_s;
-    const Stretch<BF16> st(a.logits, row + id0, n);
-    grad_stretch<BF16, false>(st, slope(m, l, a.c, out, 0.f), a.grad, r * a.grad_stride + id0);
-    grad_of_s<BF16>(a, r, t, slope(m, l, a.c, in_s, 0.f), x, id0, n);
+    Given G;
+    Entries E;
+    entries_load(a, tr, G);
+    entries_place<NT, U>(a, row, G, E);
+    if (threadIdx.x < 64) {
+        float xs[SLOTS];
+        s_elems<BF16>(row, G, xs);  // (outside this part they may be gradients by now, and are not looked at)
+        teacher_probs(a, lse, G, xs, t);
+    }
+    __syncthreads();
+    const float in_s = w * (t.P + t.rest), out = tail > -INFINITY ? in_s - w * t.rest * expf(-tail) : in_s;
+    grad_goes(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first,
+              min(first + a.part_goes, row.template goes<STREAM_GO>()), part == 0);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.
 //     d / dx_j = 1 / T [ g_lp (1[j = y] - q_j) - g_H q_j (log q_j + H) ]
 template <bool BF16, bool ENT>
-__global__ __launch_bounds__(VR_NT) void logprob_grad_kernel(LogprobGradArgs a) {
-    const int64_t r = blockIdx.x, row = r * a.row_stride;
-    const int id0 = blockIdx.y * a.part_elems, n = min(a.V - id0, a.part_elems);
+__global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    const int64_t r = blockIdx.x, at = r * a.grad_stride;
+    const int part = blockIdx.y, first = part * a.part_goes;
+    const Row<BF16> row(a.logits, r * a.row_stride, a.V);
     const int y = a.tokens ? a.tokens[r] : -1;
     const float g = y >= 0 && y < a.V && a.g_logprob ? a.g_logprob[r] * a.inv_t : 0.f;
     const float h = ENT ? a.g_entropy[r] * a.inv_t : 0.f;
     const Slope k = slope(a.stats[2 * r], a.stats[2 * r + 1], a.c, ENT ? -fmaf(h, a.entropy[r], g) : -g, -h * LN2);
-    const bool here = g != 0.f && y >= id0 && y < id0 + n;
-    const float x = here ? elem_of<BF16>(a.logits, row + y) : 0.f;
-    const Stretch<BF16> st(a.logits, row + id0, n);
-    grad_stretch<BF16, ENT>(st, k, a.grad, r * a.grad_stride + id0);
-    if (here) {  // the same for all threads
-        __syncthreads();
-        if (threadIdx.x == 0) put_elem<BF16>(a.grad, r * a.grad_stride + y, slope_at<ENT>(k, x) + g);
+    Place here = {-2, 0, 0};
+    float xy = 0.f;
+    if (g != 0.f) {
+        here = place_of<BF16, NT, U>(row, y);
+        if ((int)threadIdx.x == here.thread) xy = row.at(y);  // (before this thread stores anything)
+    }
+    const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
+    for (int it = first; it < end; ++it) {
+        Raw<BF16, U> raw;
+        go_request<NT, false>(row, it, raw);
+        float x[8 * U];
+        go_finish<NT>(row, it, raw, x);
+        put_go<NT, ENT>(row, it, k, a.grad, at, x);
+        if (it == here.go && (int)threadIdx.x == here.thread) put_elem<BF16>(a.grad, at + y, slope_at<ENT>(k, xy) + g);
+    }
+    if (part == 0 && (int)threadIdx.x < row.loose) {
+        const int i = row.loose_at(threadIdx.x);
+        float d = slope_at<ENT>(k, row.at(i));
+        if (here.go == -1 && (int)threadIdx.x == here.thread) d += g;
+        put_elem<BF16>(a.grad, at + i, d);
     }
 }
-
-static size_t marks_bytes(int elems) { return ((size_t)(elems + VR_GO_ELEMS - 1) / VR_GO_ELEMS * VR_NT + 1) * 4; }
 
 template <bool BF16, bool GRAD>
 static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
-    if (a.parts == 1) {
-        launch_kernel(KID_DISTILL, st, distill_row_kernel<BF16, GRAD>, dim3((u32)a.n), dim3(VR_NT), marks_bytes(a.V), a);
+    if (rows_held(a.V)) {
+        by_held_threads(a.V, [&](auto nt) {
+            constexpr int NT = decltype(nt)::value;
+            launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT>, dim3((u32)a.n), dim3(NT), 0, a);
+        });
         return hipGetLastError();
     }
-    launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16>, dim3((u32)a.n, a.parts), dim3(VR_NT), marks_bytes(a.part_elems), a);
+    if (a.parts == 1) {
+        launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, GRAD>, dim3((u32)a.n), dim3(STREAM_NT), 0, a);
+        return hipGetLastError();
+    }
+    launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16>, dim3((u32)a.n, a.parts), dim3(STREAM_NT), 0, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16, GRAD>, dim3((u32)a.n, GRAD ? a.parts : 1), dim3(VR_NT), 0, a);
+    launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16, GRAD>, dim3((u32)a.n, GRAD ? a.parts : 1), dim3(STREAM_NT), 0, a);
     return hipGetLastError();
 }
 
-size_t distill_workspace(int64_t n, int V) { return (size_t)n * (vocab_parts(n, V) * sizeof(float2) + DT_DISTILL_K_MAX * sizeof(float)); }
+size_t distill_workspace(int64_t n, int V) {
+    if (rows_held(V) || row_parts(n, V) == 1) return 0;
+    return (size_t)n * (row_parts(n, V) * sizeof(float2) + DT_DISTILL_K_MAX * sizeof(float));
+}
 hipError_t distill_launch(DistillArgs a, hipStream_t st) {
-    a.part_elems = vocab_part_goes(a.n, a.V) * VR_GO_ELEMS;
-    a.parts = vocab_parts(a.n, a.V);
+    a.part_goes = part_goes(a.n, a.V);
+    a.parts = row_parts(a.n, a.V);
     a.s_elems = (float *)((float2 *)a.ws + a.n * a.parts);
     if (a.dtype == DT_BF16) return a.grad ? launch_distill<true, true>(a, st) : launch_distill<true, false>(a, st);
     return a.grad ? launch_distill<false, true>(a, st) : launch_distill<false, false>(a, st);
 }
 hipError_t distill_grad_launch(DistillArgs a, hipStream_t st) {
-    a.part_elems = vocab_part_goes(a.n, a.V) * VR_GO_ELEMS;
-    a.parts = vocab_parts(a.n, a.V);
+    a.part_goes = part_goes(a.n, a.V);
+    a.parts = row_parts(a.n, a.V);
     const dim3 grid((u32)a.n, a.parts);
-    if (a.dtype == DT_BF16) launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<true>, grid, dim3(VR_NT), 0, a);
-    else launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<false>, grid, dim3(VR_NT), 0, a);
+    if (a.dtype == DT_BF16) launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<true>, grid, dim3(STREAM_NT), 0, a);
+    else launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<false>, grid, dim3(STREAM_NT), 0, a);
     return hipGetLastError();
 }
 template <bool BF16>
 static void launch_logprob_grad(const LogprobGradArgs &a, hipStream_t st) {
     const dim3 grid((u32)a.n, a.parts);
-    if (a.g_entropy) launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, true>, grid, dim3(VR_NT), 0, a);
-    else launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, false>, grid, dim3(VR_NT), 0, a);
+    if (a.g_entropy) launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
+    else launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
 }
 hipError_t logprob_grad_launch(LogprobGradArgs a, hipStream_t st) {
-    a.part_elems = vocab_part_goes(a.n, a.V) * VR_GO_ELEMS;
-    a.parts = vocab_parts(a.n, a.V);
+    a.part_goes = part_goes(a.n, a.V);
+    a.parts = row_parts(a.n, a.V);
     if (a.dtype == DT_BF16) launch_logprob_grad<true>(a, st);
     else launch_logprob_grad<false>(a, st);
     return hipGetLastError();

@@ -205,8 +205,8 @@ struct LogprobArgs {
     float *top_logprob;                   // [n, k]
     int32_t *top_id;
     void *ws;                             // sums of the parts of rows, then
-    unsigned long long *keys;             // [n, parts, k] their best
-    int parts, part_elems;                // set by the launch
+    uint16_t *slots;                      // [n, goes, 256] the largest of every thread's elements of a go, upper halves of ordered images
+    int goes, parts, part_goes;           // set by the launch
 };
 size_t logprob_workspace(int64_t n, int V);
 hipError_t logprob_launch(LogprobArgs a, hipStream_t st);
@@ -219,7 +219,7 @@ struct LogprobGradArgs {
     const float *stats, *entropy, *g_logprob, *g_entropy;
     float c, inv_t;
     void *grad;
-    int parts, part_elems;
+    int parts, part_goes;                                  // set by the launch
 };
 hipError_t logprob_grad_launch(LogprobGradArgs a, hipStream_t st);
 
@@ -236,7 +236,7 @@ struct DistillArgs {
     void *grad;                              // or null
     void *ws;                                // sums of the parts of rows, then
     float *s_elems;                          // [n, k] the student's logits of the teacher's tokens
-    int parts, part_elems;                   // set by the launch
+    int parts, part_goes;                    // set by the launch
 };
 size_t distill_workspace(int64_t n, int V);
 hipError_t distill_launch(DistillArgs a, hipStream_t st);

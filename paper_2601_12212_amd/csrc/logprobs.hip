@@ -3,55 +3,59 @@
 //     log-probability of y = ln 2 ((y c - M2) - log2 s),   entropy = ln 2 (log2 s - w / s),
 // both sums of terms of one sign.
 //
-// The k best: every thread leaves the largest of the 32 elements that it took at a go, as the upper half of its ordered image, in
-// shared memory.  The k-th largest of the threads' own maxima bounds the k-th largest element from below, and tightly (places
-// far apart in the row go to one thread); the few goes that reach it are read again, their elements that reach it listed, and the list ranked
-// by counting keys of (value, id).  A list that overflows (ties, a row whose best are neighbours) gives way to a radix selection over
-// the stretch, eight bits at a time, and the ties that still fit are taken in ascending id.
+// The k best: the k-th largest of the threads' own maxima (16-bit keys, the upper half of the ordered image) bounds the k-th largest element
+// from below, and tightly, since places far apart in the row go to one thread.  Where a row is streamed, every thread leaves the largest of the
+// 32 elements of a go as such a key, a `slot`; the few slots that reach the bound are read again, their elements that reach it listed, and the list
+// ranked by counting keys of (value, id).  A list that overflows (ties, a row whose best are neighbours) gives way to a radix selection over
+// the row, eight bits at a time, and the ties that still fit are taken in ascending id.
 #include "vocab_rows.hpp"
 
 namespace dt {
 
-#define LP_CAP 1024  // candidates that are listed
+#define NO_KEY 0x007Fu  // 16-bit key of -inf
 
-// The k largest (value, id) keys of a stretch, out of LDS: keys[0 .. returned count), in no order.
+template <int NT>
 struct TopRoom {
-    u32 kth;      // 16-bit key of the bound
-    u32 n;        // candidates
-    u32 hist[256];
-    u32 tm[VR_NT];  // the threads' largest, 16-bit keys
-    u32 counts[VR_NT / 64];
-    u32 prefix, need;
-    u64 keys[LP_CAP];
+    static constexpr int CAP = NT == 64 ? 256 : 1024, HITS = 256;
+    u32 n, hits, kth, need, prefix;
+    u32 tm[256];           // the threads' largest, 16-bit keys, those of several threads as one where there are more
+    u32 counts[NT / 64];
+    u32 hit[HITS];         // slots that reach the bound
+    union {
+        u64 keys[CAP];     // candidates
+        u32 hist[256];
+    };
 };
 
-__device__ __forceinline__ void top_keep(TopRoom &r, float x, int id) {
+template <int NT>
+__device__ __forceinline__ void top_keep(TopRoom<NT> &r, float x, int id) {
     const u32 at = atomicAdd(&r.n, 1u);
-    if (at < LP_CAP) r.keys[at] = make_key(x, (u32)id);
+    if (at < TopRoom<NT>::CAP) r.keys[at] = make_key(x, (u32)id);
 }
 
-// Radix selection: exactly the k best of a stretch that holds more than k candidates.  Every thread reads it element by element.
-template <bool BF16>
-__device__ __noinline__ void top_by_radix(TopRoom &r, const typename Elem<BF16>::T *p, int n, int id0, int k) {
+// Radix selection: exactly the k best of a row that holds more than k finite entries.
+template <bool BF16, int NT>
+__device__ __noinline__ void top_by_radix(TopRoom<NT> &r, const typename Elem<BF16>::T *p, int n, int k) {
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
     const u32 none = ord32(-INFINITY);
     u32 prefix = 0;
     int need = k;
     for (int shift = 24; shift >= (BF16 ? 16 : 0); shift -= 8) {
         __syncthreads();
-        r.hist[tid] = 0;
+        for (int i = tid; i < 256; i += NT) r.hist[i] = 0;
         __syncthreads();
-        for (int i0 = 0; i0 < n; i0 += VR_NT) {
+        for (int i0 = 0; i0 < n; i0 += NT) {
             const int i = i0 + tid;
             const u32 key = i < n ? ord32(Elem<BF16>::get(p + i)) : none;
             const bool in = key > none && (shift == 24 || (key ^ prefix) >> (shift + 8) == 0);
             const u32 digit = key >> shift & 255u;
-            // ties come by the thousand: what agrees with the wave's first lane is counted at once
+            // ties come by the thousand: what agrees with the first lane that counts is counted at once
             const u64 some = ballot(in);
             if (!some) continue;
-            const u32 first = (u32)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(some));
+            const int lead = __builtin_ctzll(some);
+            const u32 first = (u32)__builtin_amdgcn_readlane((int)digit, lead);
             const u64 same = ballot(in && digit == first);
-            if (lane == __builtin_ctzll(some)) atomicAdd(&r.hist[first], (u32)__popcll(same));
+            if (lane == lead) atomicAdd(&r.hist[first], (u32)__popcll(same));
             if (in && digit != first) atomicAdd(&r.hist[digit], 1u);
         }
         __syncthreads();
@@ -66,98 +70,72 @@ __device__ __noinline__ void top_by_radix(TopRoom &r, const typename Elem<BF16>:
         need = (int)r.need;
     }
     // `prefix` is the k-th best's key (its upper half for bf16), `need` of the elements that have it are among the best
+    __syncthreads();
     if (tid == 0) r.n = 0;
     int taken = 0;
-    for (int i0 = 0; i0 < n; i0 += VR_NT) {
+    for (int i0 = 0; i0 < n; i0 += NT) {
         const int i = i0 + tid;
         const float x = i < n ? Elem<BF16>::get(p + i) : -INFINITY;
         const u32 key = BF16 ? ord32(x) >> 16 << 16 : ord32(x);
+        const bool tied = key == prefix && x > -INFINITY;
+        const u64 tie = ballot(tied);
         __syncthreads();
-        if (key > prefix) top_keep(r, x, id0 + i);
-        const u64 tie = ballot(i < n && key == prefix && x > -INFINITY);
+        if (key > prefix) top_keep(r, x, i);
         if (lane == 0) r.counts[wave] = (u32)__popcll(tie);
         __syncthreads();
         int before = taken;
-        for (int w = 0; w < VR_NT / 64; ++w) {
+        for (int w = 0; w < NT / 64; ++w) {
             if (w < wave) before += (int)r.counts[w];
             taken += (int)r.counts[w];
         }
-        if (i < n && key == prefix && x > -INFINITY && before + (int)lanes_below(tie) < need) top_keep(r, x, id0 + i);
+        if (tied && before + (int)lanes_below(tie) < need) top_keep(r, x, i);
     }
     __syncthreads();
 }
 
-// slots [goes][NT]: 16-bit keys of the largest of every go; mine: of the thread's largest
-template <bool BF16>
-__device__ __forceinline__ int top_of_stretch(TopRoom &r, const Stretch<BF16> &st, const uint16_t *slots, float mine, int id0, int k) {
-    const int tid = threadIdx.x;
-    r.tm[tid] = ord32(mine) >> 16;
-    if (tid == 0) r.n = 0;
-    __syncthreads();
-    if (tid < 64) {
-        u32 key[4];
+// The bound from the maxima in tm (256, or the lanes' own with one wave), found by one wave; ends with a barrier.
+template <int NT>
+__device__ __forceinline__ u32 top_bound(TopRoom<NT> &r, float mine, int k) {
+    if constexpr (NT == 64) {
+        const u32 key[1] = {ord32(mine) >> 16};
+        return wave_kth<1>(key, k);
+    } else {
+        if (threadIdx.x < 64) {
+            u32 key[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) key[q] = r.tm[q * 64 + tid];
-        const u32 t = wave_kth<4>(key, k);
-        if (tid == 0) r.kth = t;
-    }
-    __syncthreads();
-    const u32 kth = r.kth;
-    const float edge = key_edge(kth);
-    if (tid < st.loose) {
-        const int i = st.loose_at(tid);
-        const float x = Elem<BF16>::get(st.p + i);
-        if (x >= edge && x > -INFINITY) top_keep(r, x, id0 + i);
-    }
-    if (r.tm[tid] >= kth) {
-        for (int it = 0, goes = st.goes(); it < goes; ++it) {
-            const u32 key = slots[it * VR_NT + tid];
-            if (key < kth || key <= 0x007Fu) continue;
-            for (int u = 0; u < VR_U; ++u) {
-                const int unit = it * VR_GO + u * VR_NT + tid;
-                if (unit >= st.units) break;
-                const int at = st.head + 8 * unit;
-                for (int e = 0; e < 8; ++e) {
-                    const float x = Elem<BF16>::get(st.p + at + e);
-                    if (x >= edge && x > -INFINITY) top_keep(r, x, id0 + at + e);
-                }
-            }
+            for (int q = 0; q < 4; ++q) key[q] = r.tm[q * 64 + threadIdx.x];
+            const u32 t = wave_kth<4>(key, k);
+            if (threadIdx.x == 0) r.kth = t;
         }
+        __syncthreads();
+        return r.kth;
     }
-    __syncthreads();
-    int n = (int)r.n;
-    if (n > LP_CAP) {
-        top_by_radix<BF16>(r, st.p, st.n, id0, k);
-        n = (int)r.n;
-    }
-    return n;
+}
+// a thread's maximum among those of its place, before a barrier
+template <int NT>
+__device__ __forceinline__ void top_offer(TopRoom<NT> &r, float mine) {
+    if (NT == 64) return;
+    if (NT == 256) r.tm[threadIdx.x] = ord32(mine) >> 16;
+    else atomicMax(&r.tm[threadIdx.x & 255], ord32(mine) >> 16);
 }
 
 // f(rank, key) for the k best of n keys, and f(rank, 0) for ranks that have none
-template <class F>
+template <int NT, class F>
 __device__ __forceinline__ void ranked(const u64 *keys, int n, int k, F f) {
-    for (int i = threadIdx.x; i < n; i += VR_NT) {
+    for (int i = threadIdx.x; i < n; i += NT) {
         const u64 key = keys[i];
         int rank = 0;
         for (int j = 0; j < n; ++j) rank += keys[j] > key;
         if (rank < k) f(rank, key);
     }
-    for (int i = n + (int)threadIdx.x; i < k; i += VR_NT) f(i, 0ull);
+    for (int i = n + (int)threadIdx.x; i < k; i += NT) f(i, 0ull);
 }
-
-struct Part {  // of a row, left for logprob_join_kernel
-    float m, s, w, pad;
-};
 
 // Where entry e's row starts, or -1: it has none
 __device__ __forceinline__ int64_t entry_row(const LogprobArgs &a, int64_t e) {
-    const int64_t b = e / a.per_seq;
-    const int64_t s = a.row_of ? (int64_t)a.row_of[e] : e - b * a.per_seq;
+    const u32 b = (u32)e / (u32)a.per_seq;
+    const int64_t s = a.row_of ? (int64_t)a.row_of[e] : e - (int64_t)b * a.per_seq;
     return s < 0 || s >= a.rows_per_seq ? -1 : (b * a.rows_per_seq + s) * a.row_stride;
-}
-template <bool BF16>
-__device__ __forceinline__ float logit_at(const LogprobArgs &a, int64_t at) {
-    return Elem<BF16>::get((const typename Elem<BF16>::T *)a.logits + at);
 }
 __device__ __forceinline__ void entry_none(const LogprobArgs &a, int64_t e) {
     const int tid = threadIdx.x;
@@ -171,145 +149,265 @@ __device__ __forceinline__ void entry_none(const LogprobArgs &a, int64_t e) {
         a.top_id[e * a.k + tid] = -1;
     }
 }
-// thread 0: what the row's sums say
+// the given token's logit, NaN: none is given (no logit is NaN)
 template <bool BF16>
-__device__ __forceinline__ void entry_write(const LogprobArgs &a, int64_t e, int64_t at, const Sums &r, const RowStat &st) {
+__device__ __forceinline__ float token_logit(const LogprobArgs &a, int64_t e, int64_t at) {
+    const int y = a.logprob ? a.tokens[e] : -1;
+    return y >= 0 && y < a.V ? Elem<BF16>::get((const typename Elem<BF16>::T *)a.logits + at + y) : NAN;
+}
+// one thread: what the row's sums say
+__device__ __forceinline__ void entry_write(const LogprobArgs &a, int64_t e, float xy, const Sums &r, const RowStat &st) {
     a.stats[2 * e] = st.m;
     a.stats[2 * e + 1] = st.l;
     if (a.entropy) a.entropy[e] = r.s > 0.f ? (st.log2s - r.w / r.s) * LN2 : 0.f;
-    if (a.logprob) {
-        const int y = a.tokens[e];
-        a.logprob[e] = y >= 0 && y < a.V ? log_prob(logit_at<BF16>(a, at + y), st, a.c) : 0.f;
-    }
+    if (a.logprob) a.logprob[e] = xy != xy ? 0.f : log_prob(xy, st, a.c);
+}
+template <int NT>
+__device__ __forceinline__ void alternatives_write(const LogprobArgs &a, int64_t e, const TopRoom<NT> &room, int found, const RowStat &st) {
+    ranked<NT>(room.keys, found, a.k, [&](int rank, u64 key) {
+        a.top_logprob[e * a.k + rank] = key ? log_prob(key_val(key), st, a.c) : -INFINITY;
+        a.top_id[e * a.k + rank] = key ? (int)key_idx(key) : -1;
+    });
 }
 
-extern __shared__ __align__(16) unsigned char lp_lds[];
-
-template <bool BF16, bool ENT, bool TOP>
-__global__ __launch_bounds__(VR_NT) void logprob_kernel(LogprobArgs a) {
-    const int64_t e = blockIdx.x;
-    const int part = blockIdx.y, tid = threadIdx.x;
-    __shared__ Sums s_sums[VR_NT / 64];
-    TopRoom *const room = (TopRoom *)lp_lds;
-    uint16_t *const slots = (uint16_t *)(room + 1);
-    const int64_t at = entry_row(a, e);
-    if (at < 0) {
-        if (part == 0 && a.parts == 1) entry_none(a, e);
-        return;
-    }
-    const int id0 = part * a.part_elems, n = min(a.V - id0, a.part_elems);
-    const Stretch<BF16> st(a.logits, at + id0, n);
-    Sums r = {-INFINITY, 0.f, 0.f};
-    float mine = -INFINITY;
-    const int goes = st.goes();
-    for (int it = 0; it < goes; ++it) {
-        Raw<BF16> raw;
-        go_request<BF16, false>(st, it, raw);
-        float x[8 * VR_U];
-        go_finish<BF16>(st, it, raw, x);
-        const float mx = max_of(x);
-        if (TOP) {
-            slots[it * VR_NT + tid] = (uint16_t)(ord32(mx) >> 16);
-            mine = fmaxf(mine, mx);
-        }
-        sums_add<ENT>(r, x, mx, a.c);
-    }
-    if (tid < st.loose) sums_add1<ENT>(r, Elem<BF16>::get(st.p + st.loose_at(tid)), a.c);
-    r = block_sums<ENT>(r, a.c, s_sums);
-    if (a.parts == 1) {
-        const RowStat rs = row_stat(r.m, r.s, a.c);
-        if (tid == 0) entry_write<BF16>(a, e, at, r, rs);
-        if (TOP) {
-            const int found = top_of_stretch<BF16>(*room, st, slots, mine, id0, a.k);
-            ranked(room->keys, found, a.k, [&](int rank, u64 key) {
-                a.top_logprob[e * a.k + rank] = key ? log_prob(key_val(key), rs, a.c) : -INFINITY;
-                a.top_id[e * a.k + rank] = key ? (int)key_idx(key) : -1;
-            });
-        }
-    } else {
-        if (tid == 0) ((Part *)a.ws)[e * a.parts + part] = Part{r.m, r.s, r.w, 0.f};
-        if (TOP) {
-            const int found = top_of_stretch<BF16>(*room, st, slots, mine, id0, a.k);
-            u64 *const out = a.keys + (e * a.parts + part) * a.k;
-            ranked(room->keys, found, a.k, [&](int rank, u64 key) { out[rank] = key; });
-        }
-    }
-}
-
-// The parts of a row (up to 64) together.
-template <bool BF16>
-__global__ __launch_bounds__(VR_NT) void logprob_join_kernel(LogprobArgs a) {
+// ---- rows that a workgroup holds ----
+template <bool BF16, bool ENT, bool TOP, int NT>
+__global__ __launch_bounds__(NT, 8) void logprob_held_kernel(LogprobArgs a) {
+    constexpr int U = 4;
     const int64_t e = blockIdx.x;
     const int tid = threadIdx.x;
+    __shared__ Sums s_sums[NT / 64];
+    __shared__ TopRoom<TOP ? NT : 64> room_;
+    TopRoom<NT> &room = (TopRoom<NT> &)room_;
     const int64_t at = entry_row(a, e);
     if (at < 0) {
         entry_none(a, e);
         return;
     }
-    u64 *const keys = (u64 *)lp_lds;
-    const int n = a.parts * a.k;
-    for (int i = tid; i < n; i += VR_NT) keys[i] = a.keys[e * n + i];
-    Sums r = {-INFINITY, 0.f, 0.f};
-    if ((tid & 63) < a.parts) {
-        const Part p = ((const Part *)a.ws)[e * a.parts + (tid & 63)];
-        r = Sums{p.m, p.s, p.w};
-    }
-    sums_move<true>(r, wave_max(r.m), a.c);
-    r.s = wave_sum(r.s);
-    r.w = wave_sum(r.w);
-    const RowStat rs = row_stat(r.m, r.s, a.c);
-    if (tid == 0) entry_write<BF16>(a, e, at, r, rs);
-    if (n == 0) return;
-    __syncthreads();
-    int mine = 0;  // keys of nothing come last: among them the order does not matter, but every rank below k is written once
-    for (int i = tid; i < n; i += VR_NT) mine += keys[i] != 0;
-    __shared__ int s_n[VR_NT / 64];
-    mine = wave_sum_i32(mine);
-    if (lane_id() == 0) s_n[tid >> 6] = mine;
-    __syncthreads();
-    int found = 0;
-    for (int i = 0; i < VR_NT / 64; ++i) found += s_n[i];
-    for (int i = tid; i < n; i += VR_NT) {
-        const u64 key = keys[i];
-        if (!key) continue;
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > key;
-        if (rank < a.k) {
-            a.top_logprob[e * a.k + rank] = log_prob(key_val(key), rs, a.c);
-            a.top_id[e * a.k + rank] = (int)key_idx(key);
+    const Row<BF16> row(a.logits, at, a.V);
+    Raw<BF16, U> raw;
+    if (row.units > 0) go_request<NT, false>(row, 0, raw);
+    const float xl = tid < row.loose ? row.at(row.loose_at(tid)) : -INFINITY;
+    const float xy = token_logit<BF16>(a, e, at);
+    if (TOP) {
+        if (tid == 0) room.n = 0;
+        if (NT > 256) {
+            if (tid < 256) room.tm[tid] = NO_KEY;
+            __syncthreads();
         }
     }
-    for (int i = found + tid; i < a.k; i += VR_NT) {
-        a.top_logprob[e * a.k + i] = -INFINITY;
-        a.top_id[e * a.k + i] = -1;
+    float x[8 * U];
+    go_finish<NT>(row, 0, raw, x);  // (no units: all -inf)
+    const float mx = max_of(x), mine = fmaxf(mx, xl);
+    Sums r = {-INFINITY, 0.f, 0.f};
+    sums_add<ENT>(r, x, mx, a.c);
+    if (row.loose > 0) sums_add1<ENT>(r, xl, a.c);  // uniform
+    if (TOP) top_offer<NT>(room, mine);
+    r = block_sums<ENT, NT>(r, a.c, s_sums);
+    const RowStat st = row_stat(r.m, r.s, a.c);
+    if (tid == NT - 1) entry_write(a, e, xy, r, st);
+    if (!TOP) return;
+    const float edge = key_edge(top_bound<NT>(room, mine, a.k));
+    if (mine >= edge && mine > -INFINITY) {
+        if (xl >= edge && xl > -INFINITY) top_keep(room, xl, row.loose_at(tid));
+#pragma unroll
+        for (int j = 0; j < 8 * U; ++j)
+            if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], row.head + 8 * ((j / 8) * NT + tid) + j % 8);
     }
+    __syncthreads();
+    int found = (int)room.n;
+    if (found > TopRoom<NT>::CAP) {
+        top_by_radix<BF16, NT>(room, row.p, a.V, a.k);
+        found = (int)room.n;
+    }
+    alternatives_write<NT>(a, e, room, found, st);
+}
+
+// ---- rows that are streamed ----
+struct Part {  // of a row, left for logprob_join_kernel
+    float m, s, w, pad;
+};
+extern __shared__ __align__(16) unsigned char lp_lds[];
+
+// The candidates among the slots that reach the bound: slot i of the row is go i / NT, thread i % NT.  Ends with a barrier; the number found.
+template <bool BF16, class Slot>
+__device__ __forceinline__ int top_of_slots(TopRoom<STREAM_NT> &r, const Row<BF16> &row, int k, float mine, Slot slot) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    typedef TopRoom<NT> R;
+    const int tid = threadIdx.x, goes = row.template goes<STREAM_GO>();
+    const u32 kth = top_bound<NT>(r, mine, k);
+    const float edge = key_edge(kth);
+    if (r.tm[tid] >= kth)
+        for (int it = 0; it < goes; ++it) {
+            const u32 key = slot(it);
+            if (key >= kth && key > NO_KEY) {
+                const u32 at = atomicAdd(&r.hits, 1u);
+                if (at < R::HITS) r.hit[at] = (u32)(it * NT + tid);
+            }
+        }
+    if (tid < row.loose) {
+        const int i = row.loose_at(tid);
+        const float x = row.at(i);
+        if (x >= edge && x > -INFINITY) top_keep(r, x, i);
+    }
+    __syncthreads();
+    const int hits = (int)r.hits;
+    if (hits <= R::HITS)
+        for (int i = tid; i < hits * U; i += NT) {  // a unit to a thread
+            const int s = (int)r.hit[i / U], unit = ((s / NT) * U + i % U) * NT + s % NT;
+            if (unit >= row.units) continue;
+            const int at = row.head + 8 * unit;
+            float x[8];
+            const Vec16 *q = (const Vec16 *)(row.p + at);
+            const Vec16 lo = q[0], hi = BF16 ? lo : q[1];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (BF16) {
+                    x[2 * j] = __uint_as_float(lo[j] << 16);
+                    x[2 * j + 1] = __uint_as_float(lo[j] & 0xFFFF0000u);
+                } else {
+                    x[j] = __uint_as_float(lo[j]);
+                    x[4 + j] = __uint_as_float(hi[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (x[j] >= edge && x[j] > -INFINITY) top_keep(r, x[j], at + j);
+        }
+    __syncthreads();
+    if (hits <= R::HITS && (int)r.n <= R::CAP) return (int)r.n;
+    top_by_radix<BF16, NT>(r, row.p, row.V, k);
+    return (int)r.n;
+}
+
+// Goes of a row, from part * part_goes on: all of them (JOIN false) or a part's, for logprob_join_kernel.
+template <bool BF16, bool ENT, bool TOP, bool JOIN>
+__global__ __launch_bounds__(STREAM_NT) void logprob_stream_kernel(LogprobArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U;
+    const int64_t e = blockIdx.x;
+    const int part = blockIdx.y, tid = threadIdx.x;
+    __shared__ Sums s_sums[NT / 64];
+    TopRoom<NT> &room = *(TopRoom<NT> *)lp_lds;  // TOP && !JOIN, and behind it the slots
+    uint16_t *const slots = JOIN ? a.slots + (e * a.goes) * NT + tid : (uint16_t *)(&room + 1) + tid;
+    const int64_t at = entry_row(a, e);
+    if (at < 0) {
+        if (!JOIN) entry_none(a, e);
+        return;
+    }
+    const Row<BF16> row(a.logits, at, a.V);
+    const float xy = JOIN ? 0.f : token_logit<BF16>(a, e, at);
+    if (TOP && !JOIN && tid == 0) room.n = room.hits = 0;
+    Sums r = {-INFINITY, 0.f, 0.f};
+    float mine = -INFINITY;
+    const int end = JOIN ? min((part + 1) * a.part_goes, row.template goes<STREAM_GO>()) : row.template goes<STREAM_GO>();
+    for (int it = JOIN ? part * a.part_goes : 0; it < end; ++it) {
+        Raw<BF16, U> raw;
+        go_request<NT, false>(row, it, raw);
+        float x[8 * U];
+        go_finish<NT>(row, it, raw, x);
+        const float mx = max_of(x);
+        if (TOP) {
+            slots[it * NT] = (uint16_t)(ord32(mx) >> 16);
+            mine = fmaxf(mine, mx);
+        }
+        sums_add<ENT>(r, x, mx, a.c);
+    }
+    if (part == 0 && tid < row.loose) sums_add1<ENT>(r, row.at(row.loose_at(tid)), a.c);
+    if (TOP && !JOIN) top_offer<NT>(room, mine);
+    r = block_sums<ENT, NT>(r, a.c, s_sums);
+    if (JOIN) {
+        if (tid == 0) ((Part *)a.ws)[e * a.parts + part] = Part{r.m, r.s, r.w, 0.f};
+        return;
+    }
+    const RowStat st = row_stat(r.m, r.s, a.c);
+    if (tid == NT - 1) entry_write(a, e, xy, r, st);
+    if (TOP) {
+        const int found = top_of_slots<BF16>(room, row, a.k, mine, [&](int it) { return (u32)slots[it * NT]; });
+        alternatives_write<NT>(a, e, room, found, st);
+    }
+}
+
+// The parts of a row together.
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(STREAM_NT, 4) void logprob_join_kernel(LogprobArgs a) {
+    constexpr int NT = STREAM_NT;
+    const int64_t e = blockIdx.x;
+    const int tid = threadIdx.x;
+    TopRoom<NT> &room = *(TopRoom<NT> *)lp_lds;  // TOP, and behind it the slots
+    uint16_t *const slots = (uint16_t *)(&room + 1);
+    const int64_t at = entry_row(a, e);
+    if (at < 0) {
+        entry_none(a, e);
+        return;
+    }
+    const Row<BF16> row(a.logits, at, a.V);
+    const float xy = token_logit<BF16>(a, e, at);
+    Sums r = {-INFINITY, 0.f, 0.f};
+    if (lane_id() < a.parts) {
+        const Part p = ((const Part *)a.ws)[e * a.parts + lane_id()];
+        r = Sums{p.m, p.s, p.w};
+    }
+    const int goes = row.template goes<STREAM_GO>();
+    if (TOP) {
+        if (tid == 0) room.n = room.hits = 0;
+        constexpr int MOST = (DT_VOCAB_MAX / STREAM_ELEMS * NT * 2 / 16 + NT - 1) / NT;
+        const Vec16 *const from = (const Vec16 *)(a.slots + e * a.goes * NT);
+        Vec16 v[MOST];
+#pragma unroll
+        for (int i = 0; i < MOST; ++i)
+            if (i * NT + tid < goes * NT / 8) v[i] = from[i * NT + tid];
+#pragma unroll
+        for (int i = 0; i < MOST; ++i)
+            if (i * NT + tid < goes * NT / 8) ((Vec16 *)slots)[i * NT + tid] = v[i];
+    }
+    wave_sums<true>(r, a.c);
+    const RowStat st = row_stat(r.m, r.s, a.c);
+    if (tid == NT - 1) entry_write(a, e, xy, r, st);
+    if (!TOP) return;
+    __syncthreads();
+    u32 best = NO_KEY;
+    for (int it = 0; it < goes; ++it) best = max(best, (u32)slots[it * NT + tid]);
+    room.tm[tid] = best;
+    __syncthreads();
+    const int found = top_of_slots<BF16>(room, row, a.k, 0.f, [&](int it) { return (u32)slots[it * NT + tid]; });
+    alternatives_write<NT>(a, e, room, found, st);
 }
 
 template <bool BF16, bool ENT, bool TOP>
 static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
-    const int goes = (a.part_elems + VR_GO_ELEMS - 1) / VR_GO_ELEMS;
-    const size_t lds = TOP ? sizeof(TopRoom) + (size_t)goes * VR_NT * 2 : 0;
-    launch_kernel(KID_LOGPROBS, st, logprob_kernel<BF16, ENT, TOP>, dim3((u32)a.n, a.parts), dim3(VR_NT), lds, a);
+    if (rows_held(a.V)) {
+        by_held_threads(a.V, [&](auto nt) {
+            constexpr int NT = decltype(nt)::value;
+            launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT>, dim3((u32)a.n), dim3(NT), 0, a);
+        });
+        return hipGetLastError();
+    }
+    const size_t lds = TOP ? sizeof(TopRoom<STREAM_NT>) + (size_t)a.goes * STREAM_NT * 2 : 0;
+    if (a.parts == 1) {
+        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false>, dim3((u32)a.n), dim3(STREAM_NT), lds, a);
+    } else {
+        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, true>, dim3((u32)a.n, a.parts), dim3(STREAM_NT), 0, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        launch_kernel(KID_LOGPROBS_JOIN, st, logprob_join_kernel<BF16, TOP>, dim3((u32)a.n), dim3(STREAM_NT), lds, a);
+    }
     return hipGetLastError();
 }
 template <bool BF16>
 static hipError_t launch_type(const LogprobArgs &a, hipStream_t st) {
-    hipError_t e;
-    if (a.entropy) e = a.k ? launch_rows<BF16, true, true>(a, st) : launch_rows<BF16, true, false>(a, st);
-    else e = a.k ? launch_rows<BF16, false, true>(a, st) : launch_rows<BF16, false, false>(a, st);
-    if (e != hipSuccess || a.parts == 1) return e;
-    launch_kernel(KID_LOGPROBS_JOIN, st, logprob_join_kernel<BF16>, dim3((u32)a.n), dim3(VR_NT), (size_t)a.parts * a.k * 8, a);
-    return hipGetLastError();
+    if (a.entropy) return a.k ? launch_rows<BF16, true, true>(a, st) : launch_rows<BF16, true, false>(a, st);
+    return a.k ? launch_rows<BF16, false, true>(a, st) : launch_rows<BF16, false, false>(a, st);
 }
 
 size_t logprob_workspace(int64_t n, int V) {
-    const int64_t parts = n * vocab_parts(n, V);
-    return (size_t)parts * (sizeof(Part) + DT_K_MAX * 8);
+    if (rows_held(V) || row_parts(n, V) == 1) return 0;
+    return (size_t)n * row_parts(n, V) * sizeof(Part) + (size_t)n * row_goes(V) * STREAM_NT * 2;
 }
 hipError_t logprob_launch(LogprobArgs a, hipStream_t st) {
-    a.part_elems = vocab_part_goes(a.n, a.V) * VR_GO_ELEMS;
-    a.parts = vocab_parts(a.n, a.V);
-    a.keys = (u64 *)((Part *)a.ws + a.n * a.parts);
+    a.goes = row_goes(a.V);
+    a.part_goes = part_goes(a.n, a.V);
+    a.parts = row_parts(a.n, a.V);
+    a.slots = (uint16_t *)((Part *)a.ws + a.n * a.parts);
     return a.dtype == DT_BF16 ? launch_type<true>(a, st) : launch_type<false>(a, st);
 }
 

@@ -1,24 +1,21 @@
-// One workgroup's pass over a stretch of a row of logits: what the log-probabilities (logprobs.hip) and the losses and gradients
-// (distill.hip) share.
+// A workgroup's pass over a row of logits: what the log-probabilities (logprobs.hip) and the losses and gradients (distill.hip) share.
 //
-// A stretch is n elements from `p` on, of any alignment.  Elements up to the first multiple of 16 bytes and behind the last whole
-// unit of eight are `loose`, up to 14, one to a thread; the units are read 16 bytes at a time.  A thread takes U units at a go, NT
-// units apart, so that a go of the workgroup reads NT * U * 8 elements front to back.
+// A row is V elements from any address.  Elements up to the first multiple of 16 bytes and behind the last whole unit of eight are `loose`, up to 14, one
+// to a thread; the units are read 16 bytes at a time.  A thread takes U units at a go, NT units apart, so that a go of a workgroup of NT threads reads
+// NT * U * 8 elements front to back.
 //
 // Softmax statistics.  With c = log2(e) / T a row's weights are 2^(x c - M2), M2 = fl(m c) for the largest logit m so far: one fused multiply-add
 // and one exp2 an element, and since every sum refers to the M2 that was subtracted, its rounding drops out of all results.  Sums are fp32.
 // Where that rounding is itself a large power (|m c| from 2^20 on, up to rows that hold nothing but masks of the type's lowest value)
 // the exponent is (x - m) c.
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 #include "kernels.hpp"
 
 namespace dt {
 
-#define VR_NT 256              // threads of a workgroup
-#define VR_U 4                 // units of a thread at a go
-#define VR_GO (VR_NT * VR_U)   // units of a go
-#define VR_GO_ELEMS (8 * VR_GO)
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.4426950408889634074f;
 
 template <bool BF16>
@@ -35,44 +32,58 @@ struct Elem<false> {
 };
 
 template <bool BF16>
-struct Stretch {
+struct Row {
     const typename Elem<BF16>::T *p;
-    int n, head, units, loose;
-    __device__ __forceinline__ Stretch(const void *logits, int64_t at, int count) {
+    int V, head, units, loose;
+    __device__ __forceinline__ Row(const void *logits, int64_t at, int n) {
         p = (const typename Elem<BF16>::T *)logits + at;
-        n = count;
+        V = n;
         const int per16 = BF16 ? 8 : 4;
         head = min((int)(-(uintptr_t)p / sizeof(*p)) & (per16 - 1), n);
         units = (n - head) >> 3;
         loose = n - 8 * units;
     }
-    // where loose element i, i < loose, lies in the stretch
+    __device__ __forceinline__ float at(int i) const { return Elem<BF16>::get(p + i); }
+    // where loose element i, i < loose, lies in the row
     __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + 8 * units; }
-    __device__ __forceinline__ int goes() const { return (units + VR_GO - 1) / VR_GO; }
+    template <int GO>
+    __device__ __forceinline__ int goes() const { return (units + GO - 1) / GO; }
 };
 
-typedef u32 Vec16 __attribute__((ext_vector_type(4)));
-template <bool BF16>
-struct Raw {
-    Vec16 r[VR_U][BF16 ? 1 : 2];
+// Where element `id` is worked on: at go `go` (-1: a loose one) by thread `thread`, as its element `elem`.
+struct Place {
+    int go, thread, elem;
 };
-// the units of go `it` of this thread; those past the end are the last unit again
-template <bool BF16, bool KEEP>
-__device__ __forceinline__ void go_request(const Stretch<BF16> &st, int it, Raw<BF16> &raw) {
+template <bool BF16, int NT, int U>
+__device__ __forceinline__ Place place_of(const Row<BF16> &row, int id) {
+    const u32 at = (u32)(id - row.head);
+    if (at >= 8u * (u32)row.units) return Place{-1, id < row.head ? id : id - 8 * row.units, 0};
+    const u32 unit = at >> 3, in_go = unit % (NT * U);
+    return Place{(int)(unit / (NT * U)), (int)(in_go % NT), (int)(8 * (in_go / NT) + (at & 7))};
+}
+
+typedef u32 Vec16 __attribute__((ext_vector_type(4)));
+template <bool BF16, int U>
+struct Raw {
+    Vec16 r[U][BF16 ? 1 : 2];
+};
+// the units of go `it` of this thread; those past the end are the last unit again (row.units > 0)
+template <int NT, bool KEEP, bool BF16, int U>
+__device__ __forceinline__ void go_request(const Row<BF16> &row, int it, Raw<BF16, U> &raw) {
 #pragma unroll
-    for (int u = 0; u < VR_U; ++u) {
-        const int unit = min(it * VR_GO + u * VR_NT + (int)threadIdx.x, st.units - 1);
-        const Vec16 *q = (const Vec16 *)(st.p + st.head + 8 * (int64_t)unit);
+    for (int u = 0; u < U; ++u) {
+        const int unit = min((it * U + u) * NT + (int)threadIdx.x, row.units - 1);
+        const Vec16 *q = (const Vec16 *)(row.p + row.head + 8 * (int64_t)unit);
 #pragma unroll
         for (int h = 0; h < (BF16 ? 1 : 2); ++h) raw.r[u][h] = KEEP ? q[h] : __builtin_nontemporal_load(q + h);
     }
     __builtin_amdgcn_sched_barrier(0);  // all on their way before anything that follows
 }
 // what was read, as floats; of units past the end -inf
-template <bool BF16>
-__device__ __forceinline__ void go_finish(const Stretch<BF16> &st, int it, const Raw<BF16> &raw, float (&x)[8 * VR_U]) {
+template <int NT, bool BF16, int U>
+__device__ __forceinline__ void go_finish(const Row<BF16> &row, int it, const Raw<BF16, U> &raw, float (&x)[8 * U]) {
 #pragma unroll
-    for (int u = 0; u < VR_U; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if constexpr (BF16) {
@@ -83,10 +94,10 @@ __device__ __forceinline__ void go_finish(const Stretch<BF16> &st, int it, const
                 x[8 * u + 4 + e] = __uint_as_float(raw.r[u][1][e]);
             }
         }
-    if ((it + 1) * VR_GO > st.units) {  // uniform
+    if ((it + 1) * NT * U > row.units) {  // uniform
 #pragma unroll
-        for (int u = 0; u < VR_U; ++u) {
-            const bool there = it * VR_GO + u * VR_NT + (int)threadIdx.x < st.units;
+        for (int u = 0; u < U; ++u) {
+            const bool there = (it * U + u) * NT + (int)threadIdx.x < row.units;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[8 * u + e] = there ? x[8 * u + e] : -INFINITY;
         }
@@ -129,21 +140,21 @@ __device__ __forceinline__ float log2_weight(float x, float m, float c) {
     const float M2 = m * c;
     return plain_ref(M2) ? fmaf(x, c, -M2) : x == m ? 0.f : (x - m) * c;
 }
-template <bool ENT>
-__device__ __forceinline__ void sums_add(Sums &a, const float (&x)[8 * VR_U], float mx, float c) {
+template <bool ENT, int N>
+__device__ __forceinline__ void sums_add(Sums &a, const float (&x)[N], float mx, float c) {
     if (mx > a.m) sums_move<ENT>(a, mx, c);
     if (a.m == -INFINITY) return;
     const float M2 = a.m * c;
     if (plain_ref(M2)) {
 #pragma unroll
-        for (int j = 0; j < 8 * VR_U; ++j) {
+        for (int j = 0; j < N; ++j) {
             const float t = fmaf(x[j], c, -M2), e = __builtin_amdgcn_exp2f(t);
             a.s += e;
             if (ENT) a.w = fmaf(e, fmaxf(t, -1e4f), a.w);  // (0 for a weight of 0)
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8 * VR_U; ++j) {
+        for (int j = 0; j < N; ++j) {
             const float t = x[j] == a.m ? 0.f : (x[j] - a.m) * c, e = __builtin_amdgcn_exp2f(t);
             a.s += e;
             if (ENT) a.w = fmaf(e, fmaxf(t, -1e4f), a.w);
@@ -154,32 +165,41 @@ template <bool ENT>
 __device__ __forceinline__ void sums_add1(Sums &a, float x, float c) {
     sums_join<ENT>(a, Sums{x, x == -INFINITY ? 0.f : 1.f, 0.f}, c);
 }
-__device__ __forceinline__ float max_of(const float (&x)[8 * VR_U]) {
+template <int N>
+__device__ __forceinline__ float max_of(const float (&x)[N]) {
     float mx = x[0];
 #pragma unroll
-    for (int j = 1; j < 8 * VR_U; ++j) mx = fmaxf(mx, x[j]);
+    for (int j = 1; j < N; ++j) mx = fmaxf(mx, x[j]);
     return mx;
 }
 
-// The sums of a workgroup's threads, in every thread.  Two barriers; `room` is the caller's.
+// the sums of a wave's lanes, in every lane
 template <bool ENT>
-__device__ __forceinline__ Sums block_sums(Sums a, float c, Sums (&room)[VR_NT / 64]) {
+__device__ __forceinline__ void wave_sums(Sums &a, float c) {
     sums_move<ENT>(a, wave_max(a.m), c);
     a.s = wave_sum(a.s);
     if (ENT) a.w = wave_sum(a.w);
-    __syncthreads();
+}
+// The sums of a workgroup's threads, in every thread.  `room` is written once in a kernel; the barrier is there for the caller's
+// shared memory too.
+template <bool ENT, int NT>
+__device__ __forceinline__ Sums block_sums(Sums a, float c, Sums (&room)[NT / 64]) {
+    wave_sums<ENT>(a, c);
+    if (NT == 64) {
+        __syncthreads();
+        return a;
+    }
     if (lane_id() == 0) room[threadIdx.x >> 6] = a;
     __syncthreads();
-    Sums r = room[0];
-#pragma unroll
-    for (int i = 1; i < VR_NT / 64; ++i) sums_join<ENT>(r, room[i], c);
+    Sums r = lane_id() < NT / 64 ? room[lane_id() % (NT / 64)] : Sums{-INFINITY, 0.f, 0.f};
+    wave_sums<ENT>(r, c);
     return r;
 }
 
 // What a row's sums say.
 struct RowStat {
     float m;     // largest logit
-    float log2s; // log2 of the sum against M2 = fl(m c), or against m c
+    float log2s; // log2 of the sum against its reference
     float l;     // log sum exp((x - m) / T)
 };
 __device__ __forceinline__ RowStat row_stat(float m, float s, float c) {
@@ -193,19 +213,30 @@ __device__ __forceinline__ float log_prob(float x, const RowStat &r, float c) {
     return r.m == -INFINITY ? -INFINITY : (log2_weight(x, r.m, c) - r.log2s) * LN2;
 }
 
-// How a call of n rows is cut: a part of a row, one to a workgroup, is this many goes.  Whole rows once they fill the chip with eight
-// workgroups to a compute unit, else as many parts as do, of a go at least.  VR_MOST_GOES: what the shared memory of a workgroup is sized for.
-constexpr int64_t VR_WORKGROUPS = 2048;
-constexpr int VR_MOST_GOES = 32;
-inline int vocab_part_goes(int64_t n, int V) {
-    const int goes = (V + VR_GO_ELEMS - 1) / VR_GO_ELEMS;
-    const int64_t parts = n < VR_WORKGROUPS ? (VR_WORKGROUPS + n - 1) / (n > 0 ? n : 1) : 1;
-    const int64_t per = parts >= goes ? 1 : (goes + parts - 1) / parts;
-    return (int)(per < VR_MOST_GOES ? per : VR_MOST_GOES);
+// ---- how a call of n rows is cut -------------------------------------------------------------------
+// Rows that one workgroup holds in its registers (up to HELD_V entries) are read once and take one launch.  Longer ones are streamed, whole rows to a
+// workgroup where there are enough to fill the chip (STREAM_ROWS), else parts of a row, of a go at least, that a second launch joins.
+constexpr int HELD_V = 32768;
+constexpr int STREAM_NT = 256, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
+constexpr int64_t STREAM_ROWS = 2048;
+inline bool rows_held(int V) { return V <= HELD_V; }
+inline int row_goes(int V) { return (V + STREAM_ELEMS - 1) / STREAM_ELEMS; }
+// goes of a part; parts of a row (up to 64)
+inline int part_goes(int64_t n, int V) {
+    const int goes = row_goes(V);
+    const int64_t parts = n < STREAM_ROWS ? (STREAM_ROWS + n - 1) / (n > 0 ? n : 1) : 1;
+    return parts >= goes ? 1 : (int)((goes + parts - 1) / parts);
 }
-inline int vocab_parts(int64_t n, int V) {
-    const int per = vocab_part_goes(n, V) * VR_GO_ELEMS;
-    return (V + per - 1) / per;
+inline int row_parts(int64_t n, int V) {
+    const int per = part_goes(n, V);
+    return (row_goes(V) + per - 1) / per;
+}
+// f(NT) with the threads of a workgroup that holds a row of V entries, as a compile-time constant
+template <class F>
+inline void by_held_threads(int V, F f) {
+    if (V <= 2048) f(std::integral_constant<int, 64>());
+    else if (V <= 8192) f(std::integral_constant<int, 256>());
+    else f(std::integral_constant<int, 1024>());
 }
 
 }  // namespace dt
