@@ -77,11 +77,7 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-__device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __hiloint2double(__shfl_xor(__double2hiint(v), o, 64), __shfl_xor(__double2loint(v), o, 64));
-    return v;
-}
+__device__ __forceinline__ double wave_sum_f64(double v) { return readlane_f64(wave_scan_incl_f64(v), 63); }
 // By one wave: the entries into `t`; x: the student's logits.  Probabilities in 64 bits, since 1 - P is one of them.
 __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, const Given &G, const float (&x)[SLOTS], Teacher &t) {
     const int lane = lane_id();
@@ -121,7 +117,9 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
     for (int s = 0; s < SLOTS; ++s) {
         if (s && a.k <= 64 * s) break;
         int same = 0;
-        for (int j = 0; j < a.k; ++j) same += t.id[j] == G.id[s];
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i)
+            for (int j = 0, n = min(a.k - 64 * i, 64); j < n; ++j) same += __builtin_amdgcn_readlane(G.id[i], j) == G.id[s];
         twice |= G.id[s] >= 0 && same > 1;
     }
     if (ballot(twice)) {
@@ -239,14 +237,15 @@ __device__ __forceinline__ Slope slope(float m, float l, float c, float a, float
     return m == -INFINITY ? Slope{0.f, INFINITY, c, a, b} : Slope{m, l * LOG2E, c, a, b};
 }
 // the gradients of a go, stored; at: where the row's gradient starts
-template <int NT, bool ENT, bool BF16, int N>
-__device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope &k, void *grad, int64_t at, const float (&x)[N]) {
+template <int NT, bool ENT, bool BF16, int U>
+__device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope &k, void *grad, int64_t at, const Raw<BF16, U> &raw) {
 #pragma unroll
-    for (int u = 0; u < N / 8; ++u) {
-        const int unit = (it * (N / 8) + u) * NT + (int)threadIdx.x;
-        float g[8];
+    for (int u = 0; u < U; ++u) {
+        const int unit = (it * U + u) * NT + (int)threadIdx.x;
+        float x[8], g[8];
+        go_take<NT, 1>(row, it, raw, u, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[8 * u + e]);
+        for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[e]);
         if (unit < row.units) put_unit<BF16>(grad, at + row.head + 8 * (int64_t)unit, g);
     }
 }
@@ -260,16 +259,20 @@ struct DistillSlope {
     float in_s, w;
     int64_t at;
 };
-// of a go: all as if outside S, then, by the same thread, those in S
-template <int NT, bool BF16, int N>
-__device__ __forceinline__ void distill_grad_go(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
-                                                const float (&x)[N]) {
-    put_go<NT, false>(row, it, d.out, a.grad, d.at, x);
+// of a lane's entries
+__device__ __forceinline__ void entry_grads(const Teacher &t, const DistillSlope &d, float (&g)[SLOTS]) {
     Slope in = d.out;
     in.a = d.in_s;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) g[s] = slope_at<false>(in, t.x[64 * s + lane_id()]) - d.w * t.sum[64 * s + lane_id()];
+}
+// The gradients of the go's elements in S, stored by the thread that has stored them as if they were outside.
+template <int NT, bool BF16>
+__device__ __forceinline__ void put_entries(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
+                                            const float (&g)[SLOTS]) {
     entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int, int i) {
-        const float g = slope_at<false>(in, t.x[i]) - d.w * t.sum[i];
-        if (lane_id() == lane) put_elem<BF16>(a.grad, d.at + t.id[i], g);
+        const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(i < 64 ? g[0] : g[1]), i & 63));
+        if (lane_id() == lane) put_elem<BF16>(a.grad, d.at + t.id[i], v);
     });
 }
 template <bool BF16>
@@ -281,16 +284,29 @@ __device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const R
     entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(in, x) - d.w * t.sum[i] : g; });
     if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
 }
-// v(entry) in the place of the go's elements of S
-template <int NT, int N, class V>
-__device__ __forceinline__ void replace(const DistillArgs &a, const Entries &E, int it, float (&x)[N], V v) {
-    entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int elem, int i) {
-        const float y = v(i);
-        const bool mine = lane_id() == lane;
+// a bit for each of the thread's elements of the go that are in S
+template <int NT, int U>
+struct Hidden {
+    u32 m[U / 4];
+    bool any;  // in the wave
+    __device__ __forceinline__ Hidden(const DistillArgs &a, const Entries &E, int it) : any(false) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = mine && j == elem ? y : x[j];
-    });
-}
+        for (int i = 0; i < U / 4; ++i) m[i] = 0;
+        entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int elem, int) {
+            any = true;
+#pragma unroll
+            for (int i = 0; i < U / 4; ++i) m[i] |= lane_id() == lane && elem >> 5 == i ? 1u << (elem & 31) : 0u;
+        });
+    }
+    // of units first .. first + G - 1
+    template <int G>
+    __device__ __forceinline__ void hide(int first, float (&x)[8 * G]) const {
+        if (!any) return;  // uniform
+        const u32 b = m[first / 4] >> (8 * (first % 4));
+#pragma unroll
+        for (int j = 0; j < 8 * G; ++j) x[j] = b >> j & 1 ? -INFINITY : x[j];
+    }
+};
 __device__ __forceinline__ float hide_loose(const DistillArgs &a, const Entries &E, float x) {
     if (threadIdx.x >= 64) return x;
     entries_at(a, E, -1, [&](int lane, int, int) { x = lane_id() == lane ? -INFINITY : x; });
@@ -303,9 +319,9 @@ __device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, fl
 }
 
 // ---- rows that a workgroup holds: read once ----
-template <bool BF16, bool GRAD, int NT>
-__global__ __launch_bounds__(NT, 8) void distill_held_kernel(DistillArgs a) {
-    constexpr int U = 4;
+template <bool BF16, bool GRAD, int NT, int U>
+__global__ __launch_bounds__(NT, BF16 ? 8 : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
+    constexpr int G = U == 4 ? 4 : 2;  // units that are worked on at once
     __shared__ Teacher t;
     __shared__ Sums room[NT / 64];
     const int64_t r = blockIdx.x;
@@ -318,31 +334,39 @@ __global__ __launch_bounds__(NT, 8) void distill_held_kernel(DistillArgs a) {
     const bool lead = threadIdx.x < 64;
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
-    Given G;
-    entries_load(a, tr, G);
-    Raw<BF16, U> raw;
+    Given Gv;
+    entries_load(a, tr, Gv);
+    Raw<BF16, U> raw = {};
     if (row.units > 0) go_request<NT, false>(row, 0, raw);
     const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
     Entries E;
-    entries_place<NT, U>(a, row, G, E);
+    entries_place<NT, U>(a, row, Gv, E);
     if (lead) {
         float xs[SLOTS];
-        s_elems<BF16>(row, G, xs);
-        teacher_probs(a, lse, G, xs, t);
+        s_elems<BF16>(row, Gv, xs);
+        teacher_probs(a, lse, Gv, xs, t);
     }
-    float x[8 * U];
-    go_finish<NT>(row, 0, raw, x);
-    replace<NT>(a, E, 0, x, [](int) { return -INFINITY; });
+    const Hidden<NT, U> hidden(a, E, 0);
     Sums s = {-INFINITY, 0.f, 0.f};
-    sums_add<false>(s, x, max_of(x), a.c);
+    bool zeros = false;
+#pragma unroll
+    for (int u = 0; u < U; u += G) {
+        float x[8 * G];
+        go_take<NT, G>(row, 0, raw, u, x);
+        hidden.template hide<G>(u, x);
+        sums_add<false>(s, x, max_of(x), a.c, zeros);
+    }
+    go_keep(raw);
     if (row.loose > 0) sums_add1<false>(s, hide_loose(a, E, xl), a.c);
     s = block_sums<false, NT>(s, a.c, room);
     const RowLoss R = row_loss(a, w, t, s);
     if (lead) loss_write(a, r, t, R);
     if (GRAD) {
         const DistillSlope d = {slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride};
-        replace<NT>(a, E, 0, x, [&](int i) { return t.x[i]; });
-        distill_grad_go<NT>(a, row, 0, E, t, d, x);
+        put_go<NT, false>(row, 0, d.out, a.grad, d.at, raw);
+        float g[SLOTS];
+        entry_grads(t, d, g);
+        put_entries<NT>(a, row, 0, E, t, d, g);
         distill_grad_loose(a, row, E, t, d, xl);
     }
 }
@@ -353,13 +377,14 @@ template <bool BF16, bool KEEP>
 __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF16> &row, const Entries &E, int first, int end, bool loose) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     Sums s = {-INFINITY, 0.f, 0.f};
+    bool zeros = false;
     for (int it = first; it < end; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, KEEP>(row, it, raw);
         float x[8 * U];
-        go_finish<NT>(row, it, raw, x);
-        replace<NT>(a, E, it, x, [](int) { return -INFINITY; });
-        sums_add<false>(s, x, max_of(x), a.c);
+        go_take<NT, U>(row, it, raw, 0, x);
+        Hidden<NT, U>(a, E, it).template hide<U>(0, x);
+        sums_add<false>(s, x, max_of(x), a.c, zeros);
     }
     if (loose && row.loose > 0) {
         const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
@@ -371,12 +396,13 @@ template <bool BF16>
 __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, int first, int end,
                                           bool loose) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
+    float g[SLOTS];
+    entry_grads(t, d, g);
     for (int it = first; it < end; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, false>(row, it, raw);
-        float x[8 * U];
-        go_finish<NT>(row, it, raw, x);
-        distill_grad_go<NT>(a, row, it, E, t, d, x);
+        put_go<NT, false>(row, it, d.out, a.grad, d.at, raw);
+        put_entries<NT>(a, row, it, E, t, d, g);
     }
     if (loose) {
         const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
@@ -538,9 +564,7 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
     for (int it = first; it < end; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, false>(row, it, raw);
-        float x[8 * U];
-        go_finish<NT>(row, it, raw, x);
-        put_go<NT, ENT>(row, it, k, a.grad, at, x);
+        put_go<NT, ENT>(row, it, k, a.grad, at, raw);
         if (it == here.go && (int)threadIdx.x == here.thread) put_elem<BF16>(a.grad, at + y, slope_at<ENT>(k, xy) + g);
     }
     if (part == 0 && (int)threadIdx.x < row.loose) {
@@ -554,9 +578,9 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
 template <bool BF16, bool GRAD>
 static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
     if (rows_held(a.V)) {
-        by_held_threads(a.V, [&](auto nt) {
-            constexpr int NT = decltype(nt)::value;
-            launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT>, dim3((u32)a.n), dim3(NT), 0, a);
+        by_held(a.V, [&](auto h) {
+            constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
+            launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
         });
         return hipGetLastError();
     }

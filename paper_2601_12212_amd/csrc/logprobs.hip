@@ -18,7 +18,7 @@ template <int NT>
 struct TopRoom {
     static constexpr int CAP = NT == 64 ? 256 : 1024, HITS = 256;
     u32 n, hits, kth, need, prefix;
-    u32 tm[256];           // the threads' largest, 16-bit keys, those of several threads as one where there are more
+    u32 tm[256];           // the threads' largest, 16-bit keys, two threads' as one where there are more
     u32 counts[NT / 64];
     u32 hit[HITS];         // slots that reach the bound
     union {
@@ -171,9 +171,9 @@ __device__ __forceinline__ void alternatives_write(const LogprobArgs &a, int64_t
 }
 
 // ---- rows that a workgroup holds ----
-template <bool BF16, bool ENT, bool TOP, int NT>
-__global__ __launch_bounds__(NT, 8) void logprob_held_kernel(LogprobArgs a) {
-    constexpr int U = 4;
+template <bool BF16, bool ENT, bool TOP, int NT, int U>
+__global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob_held_kernel(LogprobArgs a) {
+    constexpr int G = U == 4 ? 4 : 2;  // units that are worked on at once
     const int64_t e = blockIdx.x;
     const int tid = threadIdx.x;
     __shared__ Sums s_sums[NT / 64];
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(NT, 8) void logprob_held_kernel(LogprobArgs a) {
         return;
     }
     const Row<BF16> row(a.logits, at, a.V);
-    Raw<BF16, U> raw;
+    Raw<BF16, U> raw = {};
     if (row.units > 0) go_request<NT, false>(row, 0, raw);
     const float xl = tid < row.loose ? row.at(row.loose_at(tid)) : -INFINITY;
     const float xy = token_logit<BF16>(a, e, at);
@@ -196,11 +196,18 @@ __global__ __launch_bounds__(NT, 8) void logprob_held_kernel(LogprobArgs a) {
             __syncthreads();
         }
     }
-    float x[8 * U];
-    go_finish<NT>(row, 0, raw, x);  // (no units: all -inf)
-    const float mx = max_of(x), mine = fmaxf(mx, xl);
     Sums r = {-INFINITY, 0.f, 0.f};
-    sums_add<ENT>(r, x, mx, a.c);
+    float mine = xl;
+    bool zeros = false;
+#pragma unroll
+    for (int u = 0; u < U; u += G) {
+        float x[8 * G];
+        go_take<NT, G>(row, 0, raw, u, x);
+        const float mx = max_of(x);
+        mine = fmaxf(mine, mx);
+        sums_add<ENT>(r, x, mx, a.c, zeros);
+    }
+    go_keep(raw);
     if (row.loose > 0) sums_add1<ENT>(r, xl, a.c);  // uniform
     if (TOP) top_offer<NT>(room, mine);
     r = block_sums<ENT, NT>(r, a.c, s_sums);
@@ -211,8 +218,13 @@ __global__ __launch_bounds__(NT, 8) void logprob_held_kernel(LogprobArgs a) {
     if (mine >= edge && mine > -INFINITY) {
         if (xl >= edge && xl > -INFINITY) top_keep(room, xl, row.loose_at(tid));
 #pragma unroll
-        for (int j = 0; j < 8 * U; ++j)
-            if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], row.head + 8 * ((j / 8) * NT + tid) + j % 8);
+        for (int u = 0; u < U; ++u) {
+            float x[8];
+            go_take<NT, 1>(row, 0, raw, u, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], row.head + 8 * (u * NT + tid) + j);
+        }
     }
     __syncthreads();
     int found = (int)room.n;
@@ -300,17 +312,19 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_stream_kernel(LogprobArgs a
     Sums r = {-INFINITY, 0.f, 0.f};
     float mine = -INFINITY;
     const int end = JOIN ? min((part + 1) * a.part_goes, row.template goes<STREAM_GO>()) : row.template goes<STREAM_GO>();
-    for (int it = JOIN ? part * a.part_goes : 0; it < end; ++it) {
+    bool zeros = false;
+    int it = JOIN ? part * a.part_goes : 0;
+    for (; it < end; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, false>(row, it, raw);
         float x[8 * U];
-        go_finish<NT>(row, it, raw, x);
+        go_take<NT, U>(row, it, raw, 0, x);
         const float mx = max_of(x);
         if (TOP) {
             slots[it * NT] = (uint16_t)(ord32(mx) >> 16);
             mine = fmaxf(mine, mx);
         }
-        sums_add<ENT>(r, x, mx, a.c);
+        sums_add<ENT>(r, x, mx, a.c, zeros);
     }
     if (part == 0 && tid < row.loose) sums_add1<ENT>(r, row.at(row.loose_at(tid)), a.c);
     if (TOP && !JOIN) top_offer<NT>(room, mine);
@@ -376,9 +390,9 @@ __global__ __launch_bounds__(STREAM_NT, 4) void logprob_join_kernel(LogprobArgs 
 template <bool BF16, bool ENT, bool TOP>
 static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
     if (rows_held(a.V)) {
-        by_held_threads(a.V, [&](auto nt) {
-            constexpr int NT = decltype(nt)::value;
-            launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT>, dim3((u32)a.n), dim3(NT), 0, a);
+        by_held(a.V, [&](auto h) {
+            constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
+            launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
         });
         return hipGetLastError();
     }

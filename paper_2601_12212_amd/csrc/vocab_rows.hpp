@@ -9,6 +9,7 @@
 // Where that rounding is itself a large power (|m c| from 2^20 on, up to rows that hold nothing but masks of the type's lowest value)
 // the exponent is (x - m) c.
 #pragma once
+#include <cstdlib>
 #include <type_traits>
 
 #include "common.hpp"
@@ -79,29 +80,37 @@ __device__ __forceinline__ void go_request(const Row<BF16> &row, int it, Raw<BF1
     }
     __builtin_amdgcn_sched_barrier(0);  // all on their way before anything that follows
 }
-// what was read, as floats; of units past the end -inf
-template <int NT, bool BF16, int U>
-__device__ __forceinline__ void go_finish(const Row<BF16> &row, int it, const Raw<BF16, U> &raw, float (&x)[8 * U]) {
+// units first .. first + G - 1 of what was read, as floats; of units past the end -inf
+template <int NT, int G, bool BF16, int U>
+__device__ __forceinline__ void go_take(const Row<BF16> &row, int it, const Raw<BF16, U> &raw, int first, float (&x)[8 * G]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < G; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if constexpr (BF16) {
-                x[8 * u + 2 * e] = __uint_as_float(raw.r[u][0][e] << 16);
-                x[8 * u + 2 * e + 1] = __uint_as_float(raw.r[u][0][e] & 0xFFFF0000u);
+                x[8 * u + 2 * e] = __uint_as_float(raw.r[first + u][0][e] << 16);
+                x[8 * u + 2 * e + 1] = __uint_as_float(raw.r[first + u][0][e] & 0xFFFF0000u);
             } else {
-                x[8 * u + e] = __uint_as_float(raw.r[u][0][e]);
-                x[8 * u + 4 + e] = __uint_as_float(raw.r[u][1][e]);
+                x[8 * u + e] = __uint_as_float(raw.r[first + u][0][e]);
+                x[8 * u + 4 + e] = __uint_as_float(raw.r[first + u][1][e]);
             }
         }
-    if ((it + 1) * NT * U > row.units) {  // uniform
+    if ((it * U + first + G) * NT > row.units) {  // uniform
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool there = (it * U + u) * NT + (int)threadIdx.x < row.units;
+        for (int u = 0; u < G; ++u) {
+            const bool there = (it * U + first + u) * NT + (int)threadIdx.x < row.units;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[8 * u + e] = there ? x[8 * u + e] : -INFINITY;
         }
     }
+}
+
+// Between two passes over what was read: else the compiler keeps the first pass's floats, twice the registers of bf16 elements.
+template <bool BF16, int U>
+__device__ __forceinline__ void go_keep(Raw<BF16, U> &raw) {
+    if (BF16)
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm("" : "+v"(raw.r[u][0]));
 }
 
 // Sums of a part of a row against its largest logit m: s = sum 2^(x c - M2), w = sum 2^(x c - M2) (x c - M2).
@@ -140,37 +149,67 @@ __device__ __forceinline__ float log2_weight(float x, float m, float c) {
     const float M2 = m * c;
     return plain_ref(M2) ? fmaf(x, c, -M2) : x == m ? 0.f : (x - m) * c;
 }
+// Elements into a thread's sums; mx: their largest.  A weight of 0 has an exponent of -inf, whose share of w is no number: where a wave
+// comes upon one (`zeros`, the same for its lanes), w is summed with the exponents held above -1e4, from there on.  (Always so it is an instruction for
+// every element: 4,096 rows of 128,256 entries 169 us.)
 template <bool ENT, int N>
-__device__ __forceinline__ void sums_add(Sums &a, const float (&x)[N], float mx, float c) {
+__device__ __forceinline__ void sums_add(Sums &a, const float (&x)[N], float mx, float c, bool &zeros) {
     if (mx > a.m) sums_move<ENT>(a, mx, c);
-    if (a.m == -INFINITY) return;
-    const float M2 = a.m * c;
-    if (plain_ref(M2)) {
+    float M2 = a.m * c;
+    if (ballot(!plain_ref(M2))) {  // a wave that has met nothing finite yet, or logits out of the ordinary
+        const float m = a.m == -INFINITY ? 0.f : a.m, off = -ref_off(m, c);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const float t = fmaf(x[j], c, -M2), e = __builtin_amdgcn_exp2f(t);
-            a.s += e;
-            if (ENT) a.w = fmaf(e, fmaxf(t, -1e4f), a.w);  // (0 for a weight of 0)
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float t = x[j] == a.m ? 0.f : (x[j] - a.m) * c, e = __builtin_amdgcn_exp2f(t);
+            const float t = fmaf(x[j] - m, c, off), e = __builtin_amdgcn_exp2f(t);
             a.s += e;
             if (ENT) a.w = fmaf(e, fmaxf(t, -1e4f), a.w);
         }
+        return;
     }
+    float s[2] = {0.f, 0.f}, w[2] = {0.f, 0.f};
+    if (!ENT || !zeros) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float t = fmaf(x[j], c, -M2), e = __builtin_amdgcn_exp2f(t);
+            s[j & 1] += e;
+            if (ENT) w[j & 1] = fmaf(e, t, w[j & 1]);
+        }
+        w[0] += w[1];
+        if (ENT && ballot(w[0] != w[0])) zeros = true;
+    }
+    if (ENT && zeros) {
+        s[0] = s[1] = w[0] = 0.f;
+        asm("" : "+v"(M2));
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float t = fmaf(x[j], c, -M2), e = __builtin_amdgcn_exp2f(t);
+            s[j & 1] += e;
+            w[0] = fmaf(e, fmaxf(t, -1e4f), w[0]);
+        }
+    }
+    a.s += s[0] + s[1];
+    if (ENT) a.w += w[0];
 }
 template <bool ENT>
 __device__ __forceinline__ void sums_add1(Sums &a, float x, float c) {
     sums_join<ENT>(a, Sums{x, x == -INFINITY ? 0.f : 1.f, 0.f}, c);
 }
+// (v_max3_f32 by name: fmaxf makes every element a quiet number first, an instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 template <int N>
 __device__ __forceinline__ float max_of(const float (&x)[N]) {
-    float mx = x[0];
+    static_assert(N % 4 == 0, "pairs");
+    float p = max3(x[0], x[1], x[1]), q = max3(x[2], x[3], x[3]);
 #pragma unroll
-    for (int j = 1; j < N; ++j) mx = fmaxf(mx, x[j]);
-    return mx;
+    for (int j = 4; j < N; j += 4) {
+        p = max3(p, x[j], x[j + 1]);
+        q = max3(q, x[j + 2], x[j + 3]);
+    }
+    return max3(p, q, q);
 }
 
 // the sums of a wave's lanes, in every lane
@@ -218,25 +257,33 @@ __device__ __forceinline__ float log_prob(float x, const RowStat &r, float c) {
 // workgroup where there are enough to fill the chip (STREAM_ROWS), else parts of a row, of a go at least, that a second launch joins.
 constexpr int HELD_V = 32768;
 constexpr int STREAM_NT = 256, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
-constexpr int64_t STREAM_ROWS = 2048;
-inline bool rows_held(int V) { return V <= HELD_V; }
+inline int64_t tune(const char *n, int64_t d) { const char *e = getenv(n); return e ? atoll(e) : d; }
+inline int64_t stream_rows() { static int64_t v = tune("DT_SR", 2048); return v; }
+inline int64_t stream_wgs() { static int64_t v = tune("DT_WG", 2048); return v; }
+inline int held_v() { static int64_t v = tune("DT_HELD", HELD_V); return (int)v; }
+inline bool rows_held(int V) { return V <= held_v(); }
 inline int row_goes(int V) { return (V + STREAM_ELEMS - 1) / STREAM_ELEMS; }
 // goes of a part; parts of a row (up to 64)
 inline int part_goes(int64_t n, int V) {
     const int goes = row_goes(V);
-    const int64_t parts = n < STREAM_ROWS ? (STREAM_ROWS + n - 1) / (n > 0 ? n : 1) : 1;
+    const int64_t parts = n < stream_rows() ? (stream_wgs() + n - 1) / (n > 0 ? n : 1) : 1;
     return parts >= goes ? 1 : (int)((goes + parts - 1) / parts);
 }
 inline int row_parts(int64_t n, int V) {
     const int per = part_goes(n, V);
     return (row_goes(V) + per - 1) / per;
 }
-// f(NT) with the threads of a workgroup that holds a row of V entries, as a compile-time constant
+// Workgroups that hold a row: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries.
+template <int NT_, int U_>
+struct Held {
+    static constexpr int NT = NT_, U = U_;
+};
 template <class F>
-inline void by_held_threads(int V, F f) {
-    if (V <= 2048) f(std::integral_constant<int, 64>());
-    else if (V <= 8192) f(std::integral_constant<int, 256>());
-    else f(std::integral_constant<int, 1024>());
+inline void by_held(int V, F f) {
+    if (V <= 2048) f(Held<64, 4>());
+    else if (V <= 8192) f(Held<256, 4>());
+    else if (V <= 16384) f(Held<256, 8>());
+    else f(Held<512, 8>());
 }
 
 }  // namespace dt
