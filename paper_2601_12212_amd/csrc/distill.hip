@@ -195,13 +195,13 @@ __device__ __forceinline__ void row_loss_none(const DistillArgs &a, int64_t r) {
 }
 
 // ---- gradients ----
-__device__ __forceinline__ u32 to_bf16(float v) {  // to the nearest, ties to even: the one rounding of a gradient
-    const u32 u = __float_as_uint(v);
-    return (v != v ? 0x7FC00000u : u + 0x7FFFu + (u >> 16 & 1u)) >> 16;
-}
+// two gradients to the nearest bf16, ties to even (v_cvt_pk_bf16_f32): their one rounding
+typedef float Pair __attribute__((ext_vector_type(2)));
+typedef __bf16 PairBf16 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32 to_bf16(float lo, float hi) { return __builtin_bit_cast(u32, __builtin_convertvector((Pair{lo, hi}), PairBf16)); }
 template <bool BF16>
 __device__ __forceinline__ void put_elem(void *grad, int64_t at, float v) {
-    if (BF16) ((uint16_t *)grad)[at] = (uint16_t)to_bf16(v);
+    if (BF16) ((uint16_t *)grad)[at] = (uint16_t)to_bf16(v, v);
     else ((float *)grad)[at] = v;
 }
 typedef u32 Vec16Any2 __attribute__((ext_vector_type(4), aligned(2)));
@@ -211,7 +211,7 @@ __device__ __forceinline__ void put_unit(void *grad, int64_t at, const float *g)
     if constexpr (BF16) {
         Vec16 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = to_bf16(g[2 * e]) | to_bf16(g[2 * e + 1]) << 16;
+        for (int e = 0; e < 4; ++e) v[e] = to_bf16(g[2 * e], g[2 * e + 1]);
         __builtin_nontemporal_store(v, (Vec16Any2 *)((uint16_t *)grad + at));
     } else {
 #pragma unroll
@@ -236,19 +236,6 @@ __device__ __forceinline__ Slope slope(float m, float l, float c, float a, float
     // (nothing finite in the row: every q is 0)
     return m == -INFINITY ? Slope{0.f, INFINITY, c, a, b} : Slope{m, l * LOG2E, c, a, b};
 }
-// the gradients of a go, stored; at: where the row's gradient starts
-template <int NT, bool ENT, bool BF16, int U>
-__device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope &k, void *grad, int64_t at, const Raw<BF16, U> &raw) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int unit = (it * U + u) * NT + (int)threadIdx.x;
-        float x[8], g[8];
-        go_take<NT, 1>(row, it, raw, u, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[e]);
-        if (unit < row.units) put_unit<BF16>(grad, at + row.head + 8 * (int64_t)unit, g);
-    }
-}
 template <bool BF16>
 __device__ __forceinline__ void grad_zero(void *grad, int64_t at, int n, int nt) {
     for (int i = threadIdx.x; i < n; i += nt) put_elem<BF16>(grad, at + i, 0.f);
@@ -259,31 +246,6 @@ struct DistillSlope {
     float in_s, w;
     int64_t at;
 };
-// of a lane's entries
-__device__ __forceinline__ void entry_grads(const Teacher &t, const DistillSlope &d, float (&g)[SLOTS]) {
-    Slope in = d.out;
-    in.a = d.in_s;
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) g[s] = slope_at<false>(in, t.x[64 * s + lane_id()]) - d.w * t.sum[64 * s + lane_id()];
-}
-// The gradients of the go's elements in S, stored by the thread that has stored them as if they were outside.
-template <int NT, bool BF16>
-__device__ __forceinline__ void put_entries(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
-                                            const float (&g)[SLOTS]) {
-    entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int, int i) {
-        const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(i < 64 ? g[0] : g[1]), i & 63));
-        if (lane_id() == lane) put_elem<BF16>(a.grad, d.at + t.id[i], v);
-    });
-}
-template <bool BF16>
-__device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, float x) {
-    if (row.loose == 0 || threadIdx.x >= 64) return;
-    float g = slope_at<false>(d.out, x);
-    Slope in = d.out;
-    in.a = d.in_s;
-    entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(in, x) - d.w * t.sum[i] : g; });
-    if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
-}
 // a bit for each of the thread's elements of the go that are in S
 template <int NT, int U>
 struct Hidden {
@@ -312,6 +274,61 @@ __device__ __forceinline__ float hide_loose(const DistillArgs &a, const Entries 
     entries_at(a, E, -1, [&](int lane, int, int) { x = lane_id() == lane ? -INFINITY : x; });
     return x;
 }
+// The gradients of a go, G units at once; at: where the row's gradient starts.
+template <int NT, int G, bool ENT, bool BF16, int U>
+__device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope &k, void *grad, int64_t at, const Raw<BF16, U> &raw) {
+#pragma unroll
+    for (int first = 0; first < U; first += G) {
+        float x[8 * G];
+        go_take<NT, G>(row, it, raw, first, x);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int unit = (it * U + first + i) * NT + (int)threadIdx.x;
+            float g[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[8 * i + e]);
+            if (unit < row.units) put_unit<BF16>(grad, at + row.head + 8 * (int64_t)unit, g);
+        }
+    }
+}
+// Of a row with a teacher: all as if outside S, then those in S, by the threads that have stored them.  X: the student's logits of the entries are in
+// t.x; else they are read here, before this wave, which alone stores them, does.
+template <int NT, int G, bool X, bool BF16, int U>
+__device__ __forceinline__ void distill_put_go(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
+                                               const Raw<BF16, U> &raw) {
+    const int here = it * (NT / 64) + (threadIdx.x >> 6);
+    u64 any = 0;
+    float g[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        g[s] = 0.f;
+        if (s && a.k <= 64 * s) break;  // uniform
+        const u64 hits = ballot(E.where[s] == here);
+        any |= hits;
+        if (hits) {
+            const int i = 64 * s + lane_id();
+            Slope in = d.out;
+            in.a = d.in_s;
+            const float x = X ? t.x[i] : E.where[s] == here ? row.at(t.id[i]) : 0.f;
+            g[s] = slope_at<false>(in, x) - d.w * t.sum[i];
+        }
+    }
+    put_go<NT, G, false>(row, it, d.out, a.grad, d.at, raw);
+    if (any)
+        entries_at(a, E, here, [&](int lane, int, int i) {
+            const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(i < 64 ? g[0] : g[SLOTS - 1]), i & 63));
+            if (lane_id() == lane) put_elem<BF16>(a.grad, d.at + t.id[i], v);
+        });
+}
+template <bool BF16>
+__device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, float x) {
+    if (row.loose == 0 || threadIdx.x >= 64) return;
+    Slope in = d.out;
+    in.a = d.in_s;
+    float g = slope_at<false>(d.out, x);
+    entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(in, x) - d.w * t.sum[i] : g; });
+    if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
+}
 template <bool BF16>
 __device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, float (&x)[SLOTS]) {
 #pragma unroll
@@ -320,7 +337,7 @@ __device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, fl
 
 // ---- rows that a workgroup holds: read once ----
 template <bool BF16, bool GRAD, int NT, int U>
-__global__ __launch_bounds__(NT, BF16 ? 8 : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
+__global__ __launch_bounds__(NT, NT == 1024 ? 4 : BF16 ? 8 : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
     constexpr int G = U == 4 ? 4 : 2;  // units that are worked on at once
     __shared__ Teacher t;
     __shared__ Sums room[NT / 64];
@@ -363,10 +380,7 @@ __global__ __launch_bounds__(NT, BF16 ? 8 : U == 4 ? 6 : 4) void distill_held_ke
     if (lead) loss_write(a, r, t, R);
     if (GRAD) {
         const DistillSlope d = {slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride};
-        put_go<NT, false>(row, 0, d.out, a.grad, d.at, raw);
-        float g[SLOTS];
-        entry_grads(t, d, g);
-        put_entries<NT>(a, row, 0, E, t, d, g);
+        distill_put_go<NT, G, true>(a, row, 0, E, t, d, raw);
         distill_grad_loose(a, row, E, t, d, xl);
     }
 }
@@ -392,17 +406,13 @@ __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF1
     }
     return s;
 }
-template <bool BF16>
+template <bool X, bool BF16>
 __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, int first, int end,
-                                          bool loose) {
+                                          bool loose, Raw<BF16, STREAM_U> raw) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
-    float g[SLOTS];
-    entry_grads(t, d, g);
     for (int it = first; it < end; ++it) {
-        Raw<BF16, U> raw;
-        go_request<NT, false>(row, it, raw);
-        put_go<NT, false>(row, it, d.out, a.grad, d.at, raw);
-        put_entries<NT>(a, row, it, E, t, d, g);
+        if (it > first) go_request<NT, false>(row, it, raw);
+        distill_put_go<NT, U, X>(a, row, it, E, t, d, raw);
     }
     if (loose) {
         const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
@@ -440,7 +450,9 @@ __global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a
     s = block_sums<false, NT>(s, a.c, room);
     const RowLoss R = row_loss(a, w, t, s);
     if (lead) loss_write(a, r, t, R);
-    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true);
+    Raw<BF16, U> raw = {};
+    if (GRAD && goes > 0) go_request<NT, false>(row, 0, raw);
+    if (GRAD) grad_goes<true>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true, raw);
 }
 
 // Sums outside S of a part of a row, and from the first part the elements of S (the next launch may write their gradients over them).
@@ -448,8 +460,9 @@ template <bool BF16>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Sums room[NT / 64];
-    const int64_t r = blockIdx.x;
-    const int part = blockIdx.y, first = part * a.part_goes;
+    const RowPart rp = row_part(a.parts);
+    const int64_t r = rp.row;
+    const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
     if (tr < 0) return;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
@@ -473,8 +486,9 @@ template <bool BF16, bool GRAD>
 __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
-    const int64_t r = blockIdx.x;
-    const int part = blockIdx.y, first = part * a.part_goes;
+    const RowPart rp = row_part(GRAD ? a.parts : 1);
+    const int64_t r = rp.row;
+    const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
     const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
@@ -496,6 +510,8 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     Given G;
     Entries E;
     entries_load(a, tr, G);
+    Raw<BF16, U> raw = {};
+    if (GRAD && first < end) go_request<NT, false>(row, first, raw);
     entries_place<NT, U>(a, row, G, E);
     wave_sums<false>(out, a.c);
     if (lead) {
@@ -508,7 +524,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     else wave_sync();
     const RowLoss R = row_loss(a, w, t, out);
     if (lead && part == 0) loss_write(a, r, t, R);
-    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0);
+    if (GRAD) grad_goes<true>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0, raw);
 }
 
 // The gradient of a part of a row from what the loss has saved.
@@ -516,8 +532,9 @@ template <bool BF16>
 __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
-    const int64_t r = blockIdx.x;
-    const int part = blockIdx.y, first = part * a.part_goes;
+    const RowPart rp = row_part(a.parts);
+    const int64_t r = rp.row;
+    const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
     if (tr < 0) {
@@ -527,19 +544,20 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     }
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const float m = a.stats[2 * r], l = a.stats[2 * r + 1], tail = a.tail[r];
+    const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
     Given G;
     Entries E;
     entries_load(a, tr, G);
+    Raw<BF16, U> raw = {};
+    if (first < end) go_request<NT, false>(row, first, raw);
     entries_place<NT, U>(a, row, G, E);
     if (threadIdx.x < 64) {
-        float xs[SLOTS];
-        s_elems<BF16>(row, G, xs);  // (outside this part they may be gradients by now, and are not looked at)
-        teacher_probs(a, lse, G, xs, t);
+        const float none[SLOTS] = {};
+        teacher_probs(a, lse, G, none, t);
     }
     __syncthreads();
     const float in_s = w * (t.P + t.rest), out = tail > -INFINITY ? in_s - w * t.rest * expf(-tail) : in_s;
-    grad_goes(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first,
-              min(first + a.part_goes, row.template goes<STREAM_GO>()), part == 0);
+    grad_goes<false>(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first, end, part == 0, raw);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.
@@ -547,8 +565,9 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
 template <bool BF16, bool ENT>
 __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
-    const int64_t r = blockIdx.x, at = r * a.grad_stride;
-    const int part = blockIdx.y, first = part * a.part_goes;
+    const RowPart rp = row_part(a.parts);
+    const int64_t r = rp.row, at = r * a.grad_stride;
+    const int part = rp.part, first = part * a.part_goes;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
     const int y = a.tokens ? a.tokens[r] : -1;
     const float g = y >= 0 && y < a.V && a.g_logprob ? a.g_logprob[r] * a.inv_t : 0.f;
@@ -564,7 +583,7 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
     for (int it = first; it < end; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, false>(row, it, raw);
-        put_go<NT, ENT>(row, it, k, a.grad, at, raw);
+        put_go<NT, U, ENT>(row, it, k, a.grad, at, raw);
         if (it == here.go && (int)threadIdx.x == here.thread) put_elem<BF16>(a.grad, at + y, slope_at<ENT>(k, xy) + g);
     }
     if (part == 0 && (int)threadIdx.x < row.loose) {
@@ -584,45 +603,59 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
         });
         return hipGetLastError();
     }
+    if constexpr (GRAD)
+        if (rows_held_long(a.n, a.V, BF16)) {
+            const bool half = a.V <= 65536;
+            if (half) launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, 1024, 8>, dim3((u32)a.n), dim3(1024), 0, a);
+            else if constexpr (BF16) launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, 1024, 16>, dim3((u32)a.n), dim3(1024), 0, a);
+            return hipGetLastError();
+        }
     if (a.parts == 1) {
         launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, GRAD>, dim3((u32)a.n), dim3(STREAM_NT), 0, a);
         return hipGetLastError();
     }
-    launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16>, dim3((u32)a.n, a.parts), dim3(STREAM_NT), 0, a);
+    launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16, GRAD>, dim3((u32)a.n, GRAD ? a.parts : 1), dim3(STREAM_NT), 0, a);
+    launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16, GRAD>, dim3((u32)(GRAD ? a.n * a.parts : a.n)), dim3(STREAM_NT), 0, a);
     return hipGetLastError();
 }
 
 size_t distill_workspace(int64_t n, int V) {
-    if (rows_held(V) || row_parts(n, V) == 1) return 0;
-    return (size_t)n * (row_parts(n, V) * sizeof(float2) + DT_DISTILL_K_MAX * sizeof(float));
+    const int parts = row_parts(V, part_goes(n, V));
+    if (rows_held(V) || parts == 1) return 0;
+    return (size_t)n * (parts * sizeof(float2) + DT_DISTILL_K_MAX * sizeof(float));
 }
 hipError_t distill_launch(DistillArgs a, hipStream_t st) {
     a.part_goes = part_goes(a.n, a.V);
-    a.parts = row_parts(a.n, a.V);
+    a.parts = row_parts(a.V, a.part_goes);
     a.s_elems = (float *)((float2 *)a.ws + a.n * a.parts);
     if (a.dtype == DT_BF16) return a.grad ? launch_distill<true, true>(a, st) : launch_distill<true, false>(a, st);
     return a.grad ? launch_distill<false, true>(a, st) : launch_distill<false, false>(a, st);
 }
+// goes of a part where nothing joins the parts: a launch has up to 2^32 - 1 threads
+static int grad_goes_of(int64_t n, int V, int least) {
+    int per = least;
+    while (n * row_parts(V, per) > ((int64_t)1 << 24) - 1) ++per;
+    return per;
+}
 hipError_t distill_grad_launch(DistillArgs a, hipStream_t st) {
-    a.part_goes = part_goes(a.n, a.V);
-    a.parts = row_parts(a.n, a.V);
-    const dim3 grid((u32)a.n, a.parts);
+    a.part_goes = grad_goes_of(a.n, a.V, (int)tune("DT_DG", 1));
+    a.parts = row_parts(a.V, a.part_goes);
+    const dim3 grid((u32)(a.n * a.parts));
     if (a.dtype == DT_BF16) launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<true>, grid, dim3(STREAM_NT), 0, a);
     else launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<false>, grid, dim3(STREAM_NT), 0, a);
     return hipGetLastError();
 }
 template <bool BF16>
 static void launch_logprob_grad(const LogprobGradArgs &a, hipStream_t st) {
-    const dim3 grid((u32)a.n, a.parts);
+    const dim3 grid((u32)(a.n * a.parts));
     if (a.g_entropy) launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
     else launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
 }
 hipError_t logprob_grad_launch(LogprobGradArgs a, hipStream_t st) {
-    a.part_goes = part_goes(a.n, a.V);
-    a.parts = row_parts(a.n, a.V);
+    a.part_goes = grad_goes_of(a.n, a.V, (int)tune("DT_LG", 1));
+    a.parts = row_parts(a.V, a.part_goes);
     if (a.dtype == DT_BF16) launch_logprob_grad<true>(a, st);
     else launch_logprob_grad<false>(a, st);
     return hipGetLastError();

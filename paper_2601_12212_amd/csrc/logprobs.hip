@@ -242,14 +242,14 @@ struct Part {  // of a row, left for logprob_join_kernel
 extern __shared__ __align__(16) unsigned char lp_lds[];
 
 // The candidates among the slots that reach the bound: slot i of the row is go i / NT, thread i % NT.  Ends with a barrier; the number found.
-template <bool BF16, class Slot>
-__device__ __forceinline__ int top_of_slots(TopRoom<STREAM_NT> &r, const Row<BF16> &row, int k, float mine, Slot slot) {
-    constexpr int NT = STREAM_NT, U = STREAM_U;
+template <int NT, bool BF16, class Slot>
+__device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row, int k, float mine, Slot slot) {
+    constexpr int U = STREAM_U;
     typedef TopRoom<NT> R;
-    const int tid = threadIdx.x, goes = row.template goes<STREAM_GO>();
+    const int tid = threadIdx.x, goes = row.template goes<NT * U>();
     const u32 kth = top_bound<NT>(r, mine, k);
     const float edge = key_edge(kth);
-    if (r.tm[tid] >= kth)
+    if (r.tm[tid & 255] >= kth)
         for (int it = 0; it < goes; ++it) {
             const u32 key = slot(it);
             if (key >= kth && key > NO_KEY) {
@@ -293,11 +293,12 @@ __device__ __forceinline__ int top_of_slots(TopRoom<STREAM_NT> &r, const Row<BF1
 }
 
 // Goes of a row, from part * part_goes on: all of them (JOIN false) or a part's, for logprob_join_kernel.
-template <bool BF16, bool ENT, bool TOP, bool JOIN>
-__global__ __launch_bounds__(STREAM_NT) void logprob_stream_kernel(LogprobArgs a) {
-    constexpr int NT = STREAM_NT, U = STREAM_U;
-    const int64_t e = blockIdx.x;
-    const int part = blockIdx.y, tid = threadIdx.x;
+template <bool BF16, bool ENT, bool TOP, bool JOIN, int NT>
+__global__ __launch_bounds__(NT, 8) void logprob_stream_kernel(LogprobArgs a) {
+    constexpr int U = STREAM_U;
+    const RowPart rp = row_part(JOIN ? a.parts : 1);
+    const int64_t e = rp.row;
+    const int part = rp.part, tid = threadIdx.x;
     __shared__ Sums s_sums[NT / 64];
     TopRoom<NT> &room = *(TopRoom<NT> *)lp_lds;  // TOP && !JOIN, and behind it the slots
     uint16_t *const slots = JOIN ? a.slots + (e * a.goes) * NT + tid : (uint16_t *)(&room + 1) + tid;
@@ -308,10 +309,16 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_stream_kernel(LogprobArgs a
     }
     const Row<BF16> row(a.logits, at, a.V);
     const float xy = JOIN ? 0.f : token_logit<BF16>(a, e, at);
-    if (TOP && !JOIN && tid == 0) room.n = room.hits = 0;
+    if (TOP && !JOIN) {
+        if (tid == 0) room.n = room.hits = 0;
+        if (NT > 256) {
+            if (tid < 256) room.tm[tid] = NO_KEY;
+            __syncthreads();
+        }
+    }
     Sums r = {-INFINITY, 0.f, 0.f};
     float mine = -INFINITY;
-    const int end = JOIN ? min((part + 1) * a.part_goes, row.template goes<STREAM_GO>()) : row.template goes<STREAM_GO>();
+    const int end = JOIN ? min((part + 1) * a.part_goes, row.template goes<NT * U>()) : row.template goes<NT * U>();
     bool zeros = false;
     int it = JOIN ? part * a.part_goes : 0;
     for (; it < end; ++it) {
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_stream_kernel(LogprobArgs a
     const RowStat st = row_stat(r.m, r.s, a.c);
     if (tid == NT - 1) entry_write(a, e, xy, r, st);
     if (TOP) {
-        const int found = top_of_slots<BF16>(room, row, a.k, mine, [&](int it) { return (u32)slots[it * NT]; });
+        const int found = top_of_slots<NT, BF16>(room, row, a.k, mine, [&](int it) { return (u32)slots[it * NT]; });
         alternatives_write<NT>(a, e, room, found, st);
     }
 }
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(STREAM_NT, 4) void logprob_join_kernel(LogprobArgs 
     for (int it = 0; it < goes; ++it) best = max(best, (u32)slots[it * NT + tid]);
     room.tm[tid] = best;
     __syncthreads();
-    const int found = top_of_slots<BF16>(room, row, a.k, 0.f, [&](int it) { return (u32)slots[it * NT + tid]; });
+    const int found = top_of_slots<NT, BF16>(room, row, a.k, 0.f, [&](int it) { return (u32)slots[it * NT + tid]; });
     alternatives_write<NT>(a, e, room, found, st);
 }
 
@@ -398,9 +405,12 @@ static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
     }
     const size_t lds = TOP ? sizeof(TopRoom<STREAM_NT>) + (size_t)a.goes * STREAM_NT * 2 : 0;
     if (a.parts == 1) {
-        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false>, dim3((u32)a.n), dim3(STREAM_NT), lds, a);
+        const size_t lds4 = TOP ? sizeof(TopRoom<1024>) + (size_t)((a.V + 32767) / 32768) * 2048 : 0, lds2 = TOP ? sizeof(TopRoom<512>) + (size_t)((a.V + 16383) / 16384) * 1024 : 0;
+        if (long_nt() == 256) launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false, 256>, dim3((u32)a.n), dim3(256), lds, a);
+        else if (long_nt() == 512) launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false, 512>, dim3((u32)a.n), dim3(512), lds2, a);
+        else launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false, 1024>, dim3((u32)a.n), dim3(1024), lds4, a);
     } else {
-        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, true>, dim3((u32)a.n, a.parts), dim3(STREAM_NT), 0, a);
+        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, true, STREAM_NT>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         launch_kernel(KID_LOGPROBS_JOIN, st, logprob_join_kernel<BF16, TOP>, dim3((u32)a.n), dim3(STREAM_NT), lds, a);
@@ -414,13 +424,14 @@ static hipError_t launch_type(const LogprobArgs &a, hipStream_t st) {
 }
 
 size_t logprob_workspace(int64_t n, int V) {
-    if (rows_held(V) || row_parts(n, V) == 1) return 0;
-    return (size_t)n * row_parts(n, V) * sizeof(Part) + (size_t)n * row_goes(V) * STREAM_NT * 2;
+    const int parts = row_parts(V, part_goes(n, V));
+    if (rows_held(V) || parts == 1) return 0;
+    return (size_t)n * parts * sizeof(Part) + (size_t)n * row_goes(V) * STREAM_NT * 2;
 }
 hipError_t logprob_launch(LogprobArgs a, hipStream_t st) {
     a.goes = row_goes(a.V);
     a.part_goes = part_goes(a.n, a.V);
-    a.parts = row_parts(a.n, a.V);
+    a.parts = row_parts(a.V, a.part_goes);
     a.slots = (uint16_t *)((Part *)a.ws + a.n * a.parts);
     return a.dtype == DT_BF16 ? launch_type<true>(a, st) : launch_type<false>(a, st);
 }

@@ -96,6 +96,7 @@ __device__ __forceinline__ void go_take(const Row<BF16> &row, int it, const Raw<
             }
         }
     if ((it * U + first + G) * NT > row.units) {  // uniform
+        asm volatile("");  // (a branch, and not a choice for every element)
 #pragma unroll
         for (int u = 0; u < G; ++u) {
             const bool there = (it * U + first + u) * NT + (int)threadIdx.x < row.units;
@@ -253,15 +254,13 @@ __device__ __forceinline__ float log_prob(float x, const RowStat &r, float c) {
 }
 
 // ---- how a call of n rows is cut -------------------------------------------------------------------
-// Rows that one workgroup holds in its registers (up to HELD_V entries) are read once and take one launch.  Longer ones are streamed, whole rows to a
+// Rows that one workgroup holds in its registers are read once and take one launch.  Longer ones are streamed, whole rows to a
 // workgroup where there are enough to fill the chip (STREAM_ROWS), else parts of a row, of a go at least, that a second launch joins.
-constexpr int HELD_V = 32768;
-constexpr int STREAM_NT = 256, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
 inline int64_t tune(const char *n, int64_t d) { const char *e = getenv(n); return e ? atoll(e) : d; }
+inline int long_nt() { static int64_t v = tune("DT_NT", 256); return (int)v; }
+constexpr int STREAM_NT = 256, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
 inline int64_t stream_rows() { static int64_t v = tune("DT_SR", 2048); return v; }
 inline int64_t stream_wgs() { static int64_t v = tune("DT_WG", 2048); return v; }
-inline int held_v() { static int64_t v = tune("DT_HELD", HELD_V); return (int)v; }
-inline bool rows_held(int V) { return V <= held_v(); }
 inline int row_goes(int V) { return (V + STREAM_ELEMS - 1) / STREAM_ELEMS; }
 // goes of a part; parts of a row (up to 64)
 inline int part_goes(int64_t n, int V) {
@@ -269,11 +268,17 @@ inline int part_goes(int64_t n, int V) {
     const int64_t parts = n < stream_rows() ? (stream_wgs() + n - 1) / (n > 0 ? n : 1) : 1;
     return parts >= goes ? 1 : (int)((goes + parts - 1) / parts);
 }
-inline int row_parts(int64_t n, int V) {
-    const int per = part_goes(n, V);
-    return (row_goes(V) + per - 1) / per;
+inline int row_parts(int V, int part_goes) { return (row_goes(V) + part_goes - 1) / part_goes; }
+// Launches are lines of workgroups, the parts of a row one after the other: workgroup i is part i % parts of row i / parts.
+struct RowPart {
+    int64_t row;
+    int part;
+};
+__device__ __forceinline__ RowPart row_part(int parts) {
+    const u32 r = parts == 1 ? blockIdx.x : blockIdx.x / (u32)parts;
+    return RowPart{(int64_t)r, (int)(blockIdx.x - r * (u32)parts)};
 }
-// Workgroups that hold a row: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries.
+// Workgroups that hold a row: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries, false if none does.
 template <int NT_, int U_>
 struct Held {
     static constexpr int NT = NT_, U = U_;
@@ -285,5 +290,10 @@ inline void by_held(int V, F f) {
     else if (V <= 16384) f(Held<256, 8>());
     else f(Held<512, 8>());
 }
+constexpr int HELD_V = 32768;
+inline bool rows_held(int V) { return V <= HELD_V; }
+// Longer ones, where a gradient would read them again: up to 131,072 bf16 entries, 65,536 of fp32, in the registers of a whole compute unit.
+inline int64_t held_rows() { static int64_t v = tune("DT_HR", 512); return v; }
+inline bool rows_held_long(int64_t n, int V, bool bf16) { return n >= held_rows() && V <= (bf16 ? 131072 : 65536); }
 
 }  // namespace dt
