@@ -78,7 +78,27 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 __device__ __forceinline__ double wave_sum_f64(double v) { return readlane_f64(wave_scan_incl_f64(v), 63); }
-// By one wave: the entries into `t`; x: the student's logits.  Probabilities in 64 bits, since 1 - P is one of them.
+// exp(hi + lo) to about 2^-28, since 1 - P is one of the teacher's probabilities: e^g for g = hi + lo - n ln 2, |g| <= 0.35, as
+// 1 + g + g^2 (1/2 + g (1/6 + ...)), the sum of the first two exact.  (In 64 bits the function's constants alone, two registers each, were kept by every
+// thread for as long as its row.)
+__device__ __forceinline__ double exp_pair(float hi, float lo) {
+    if (!(hi > -104.f)) return 0.0;
+    const float n = rintf(hi * LOG2E);
+    // n ln 2 in three parts, the first two of so few digits that their products are exact
+    const float a = fmaf(n, -0.693359375f, hi), b = n * 2.12194440e-4f;  // ln 2 = 0.693359375 - 2.12194440e-4 + 1.646595e-12
+    const float c = fmaf(n, -1.646595e-12f, lo);
+    float g = a + b;
+    const float bb = g - a, e0 = (a - (g - bb)) + (b - bb);  // a + b = g + e0
+    const float low = e0 + c, v = g + low;
+    float q = fmaf(v, 1.9841270e-4f, 1.3888889e-3f);
+    q = fmaf(v, q, 8.3333333e-3f);
+    q = fmaf(v, q, 4.1666667e-2f);
+    q = fmaf(v, q, 1.6666667e-1f);
+    q = fmaf(v, q, 0.5f);
+    q = v * v * q;
+    return ldexp(1.0 + (double)g + ((double)low + (double)q), (int)n);
+}
+// By one wave: the entries into `t`; x: the student's logits.
 __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, const Given &G, const float (&x)[SLOTS], Teacher &t) {
     const int lane = lane_id();
     double P = 0.0, p[SLOTS], lp[SLOTS];
@@ -86,14 +106,16 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
     for (int s = 0; s < SLOTS; ++s) {
         p[s] = lp[s] = 0.0;
         if (G.id[s] >= 0) {
-            lp[s] = (double)G.val[s] - (double)lse;
-            p[s] = exp(lp[s]);
+            const float v = G.val[s], hi = v - lse, back = hi - v;
+            lp[s] = (double)v - (double)lse;
+            p[s] = exp_pair(hi, (v - (hi - back)) - (lse + back));
             P += p[s];
         }
     }
     P = wave_sum_f64(P);
     if ((a.flags & DT_DISTILL_RENORM) && P > 0.0) {
-        const double l = log(P);
+        const float l0 = logf((float)P);
+        const double l = (double)l0 + (P * exp_pair(-l0, 0.f) - 1.0);
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
             p[s] /= P;
@@ -351,17 +373,17 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : BF16 ? 8 : U == 4 ? 6 : 4) voi
     const bool lead = threadIdx.x < 64;
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
-    Given Gv;
-    entries_load(a, tr, Gv);
-    Raw<BF16, U> raw = {};
-    if (row.units > 0) go_request<NT, false>(row, 0, raw);
+    Given given;
+    entries_load(a, tr, given);
+    Raw<BF16, U> raw;
+    go_request<NT, false>(row, 0, raw);
     const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
     Entries E;
-    entries_place<NT, U>(a, row, Gv, E);
+    entries_place<NT, U>(a, row, given, E);
     if (lead) {
         float xs[SLOTS];
-        s_elems<BF16>(row, Gv, xs);
-        teacher_probs(a, lse, Gv, xs, t);
+        s_elems<BF16>(row, given, xs);
+        teacher_probs(a, lse, given, xs, t);
     }
     const Hidden<NT, U> hidden(a, E, 0);
     Sums s = {-INFINITY, 0.f, 0.f};
@@ -596,18 +618,18 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
 
 template <bool BF16, bool GRAD>
 static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
+    const auto held = [&](auto h) {
+        constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
+        launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
+    };
     if (rows_held(a.V)) {
-        by_held(a.V, [&](auto h) {
-            constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
-            launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
-        });
+        by_held(a.V, held);
         return hipGetLastError();
     }
     if constexpr (GRAD)
         if (rows_held_long(a.n, a.V, BF16)) {
-            const bool half = a.V <= 65536;
-            if (half) launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, 1024, 8>, dim3((u32)a.n), dim3(1024), 0, a);
-            else if constexpr (BF16) launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, 1024, 16>, dim3((u32)a.n), dim3(1024), 0, a);
+            if (a.V <= 65536) held(Held<1024, 8>());
+            else if constexpr (BF16) held(Held<1024, 16>());
             return hipGetLastError();
         }
     if (a.parts == 1) {

@@ -185,8 +185,8 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
         return;
     }
     const Row<BF16> row(a.logits, at, a.V);
-    Raw<BF16, U> raw = {};
-    if (row.units > 0) go_request<NT, false>(row, 0, raw);
+    Raw<BF16, U> raw;
+    go_request<NT, false>(row, 0, raw);
     const float xl = tid < row.loose ? row.at(row.loose_at(tid)) : -INFINITY;
     const float xy = token_logit<BF16>(a, e, at);
     if (TOP) {

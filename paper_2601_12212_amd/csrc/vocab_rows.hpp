@@ -290,8 +290,8 @@ inline void by_held(int V, F f) {
     else if (V <= 16384) f(Held<256, 8>());
     else f(Held<512, 8>());
 }
-constexpr int HELD_V = 32768;
-inline bool rows_held(int V) { return V <= HELD_V; }
+constexpr int HELD_V = 32768, HELD_LEAST = 32;  // (shorter ones may have no whole unit)
+inline bool rows_held(int V) { return V >= HELD_LEAST && V <= HELD_V; }
 // Longer ones, where a gradient would read them again: up to 131,072 bf16 entries, 65,536 of fp32, in the registers of a whole compute unit.
 inline int64_t held_rows() { static int64_t v = tune("DT_HR", 512); return v; }
 inline bool rows_held_long(int64_t n, int V, bool bf16) { return n >= held_rows() && V <= (bf16 ? 131072 : 65536); }
