@@ -9,8 +9,7 @@
 // left where the student is sure.  Outside S every gradient is q_j times one factor of the row, for log-probabilities and entropies q_j times a linear
 // function of log q_j: one exponential an element, which is read and written once by one thread, so that a gradient may take its logits' place.
 //
-// Which elements belong to S a wave knows from its lanes: lane i holds where entries i and 64 + i lie (go, thread, element of the thread), a ballot
-// at every go finds those of the wave's own, rarely one.
+// Which elements belong to S a wave knows from its lanes: lane i holds where entries i and 64 + i lie (go, thread, element of the thread).
 #include "vocab_rows.hpp"
 
 namespace dt {
@@ -22,6 +21,7 @@ struct Teacher {                       // the entries, as the first wave leaves 
     float sum[DT_DISTILL_K_MAX];       // p of all entries with the same id
     float x[DT_DISTILL_K_MAX];         // the student's logits
     int id[DT_DISTILL_K_MAX];          // -1: none
+    int found[512];                    // an entry for a hash of its id
     float P, rest, in_m, in_s;         // the student's sum in S
 };
 struct Entries {  // of a lane: where they are worked on
@@ -123,7 +123,7 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
         }
         P = 1.0;
     }
-    // sums over entries with the same id, mostly one
+    // sums over entries with the same id
     bool first[SLOTS], twice = false;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -135,14 +135,28 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
         first[s] = G.id[s] >= 0;
     }
     wave_sync();
+    // Every entry writes its number to a place that its id names; who finds another's there has the same id, or only the same place, and tries another.
+    // (Whoever is found is done, so every turn has fewer.  All ids against all: 17 us a call of few rows with 100 entries, 7.)
+    bool open[SLOTS];
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-        if (s && a.k <= 64 * s) break;
-        int same = 0;
+    for (int s = 0; s < SLOTS; ++s) open[s] = G.id[s] >= 0;
+    for (u32 by = 0x9E3779B1u;; by += 0x3C6EF372u) {
+        bool more = false;
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i)
-            for (int j = 0, n = min(a.k - 64 * i, 64); j < n; ++j) same += __builtin_amdgcn_readlane(G.id[i], j) == G.id[s];
-        twice |= G.id[s] >= 0 && same > 1;
+        for (int s = 0; s < SLOTS; ++s)
+            if (open[s]) t.found[(u32)G.id[s] * by >> 23] = 64 * s + lane;
+        wave_sync();
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (open[s]) {
+                const int other = t.found[(u32)G.id[s] * by >> 23];
+                const bool same = t.id[other] == G.id[s];
+                open[s] = !same;
+                twice |= same && other != 64 * s + lane;
+                more |= !same;
+            }
+        if (!ballot(more)) break;
+        wave_sync();
     }
     if (ballot(twice)) {
         float sum[SLOTS];
@@ -177,8 +191,8 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
 // What the second pass over a row goes by.
 struct RowLoss {
     RowStat st;
-    float tail;       // log of the probability outside S
-    float in_s, out;  // factors of q_j in S and outside, w / T in them
+    float sum_in, sum_out;  // the row's sums in S and outside
+    float in_s, out;        // factors of q_j in S and outside, w / T in them
 };
 // from the row's sums in S and outside, by any thread
 __device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, float w, const Teacher &t, Sums out) {
@@ -189,13 +203,16 @@ __device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, float w, const
     const float whole = in.s + out.s;
     RowLoss R;
     R.st = row_stat(m, whole, a.c);
-    R.tail = !(whole > 0.f) ? -INFINITY : in.s < out.s ? log1pf(-in.s / whole) : logf(out.s / whole);
+    R.sum_in = in.s;
+    R.sum_out = out.s;
     R.in_s = w * (t.P + t.rest);
     R.out = out.s > 0.f ? R.in_s - w * t.rest * (whole / out.s) : R.in_s;
     return R;
 }
 // by the first wave
 __device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, const Teacher &t, const RowLoss &R) {
+    const float whole = R.sum_in + R.sum_out;
+    const float tail = !(whole > 0.f) ? -INFINITY : R.sum_in < R.sum_out ? log1pf(-R.sum_in / whole) : logf(R.sum_out / whole);
     double term = 0.0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -203,13 +220,13 @@ __device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, cons
         const double p = t.p[i];
         if (p > 0.0) term += p * (t.lp[i] - (double)log_prob(t.x[i], R.st, a.c));
     }
-    if (lane_id() == 0 && t.rest > 0.f) term += (double)t.rest * ((double)logf(t.rest) - (double)R.tail);
+    if (lane_id() == 0 && t.rest > 0.f) term += (double)t.rest * ((double)logf(t.rest) - (double)tail);
     term = wave_sum_f64(term);
     if (lane_id() == 0) {
         a.loss[r] = (float)term;
         a.stats[2 * r] = R.st.m;
         a.stats[2 * r + 1] = R.st.l;
-        a.tail[r] = R.tail;
+        a.tail[r] = tail;
     }
 }
 __device__ __forceinline__ void row_loss_none(const DistillArgs &a, int64_t r) {
@@ -268,19 +285,31 @@ struct DistillSlope {
     float in_s, w;
     int64_t at;
 };
-// a bit for each of the thread's elements of the go that are in S
+// a bit for each of the thread's elements of the go that are in S; room: the wave's
 template <int NT, int U>
 struct Hidden {
     u32 m[U / 4];
     bool any;  // in the wave
-    __device__ __forceinline__ Hidden(const DistillArgs &a, const Entries &E, int it) : any(false) {
+    __device__ __forceinline__ Hidden(const Entries &E, int it, u32 (&room)[NT * U / 4]) : any(false) {
+        const int here = it * (NT / 64) + (threadIdx.x >> 6);
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) any |= ballot(E.where[s] == here) != 0;
 #pragma unroll
         for (int i = 0; i < U / 4; ++i) m[i] = 0;
-        entries_at(a, E, it * (NT / 64) + (threadIdx.x >> 6), [&](int lane, int elem, int) {
-            any = true;
+        if (!any) return;
+        u32 *const mine = room + (threadIdx.x >> 6) * (64 * U / 4);
 #pragma unroll
-            for (int i = 0; i < U / 4; ++i) m[i] |= lane_id() == lane && elem >> 5 == i ? 1u << (elem & 31) : 0u;
-        });
+        for (int i = 0; i < U / 4; ++i) mine[64 * i + lane_id()] = 0;
+        wave_sync();
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (E.where[s] == here) {
+                const int lane = E.which[s] & 63, elem = E.which[s] >> 6;
+                atomicOr(&mine[64 * (elem >> 5) + lane], 1u << (elem & 31));
+            }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < U / 4; ++i) m[i] = mine[64 * i + lane_id()];
     }
     // of units first .. first + G - 1
     template <int G>
@@ -313,34 +342,22 @@ __device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope
         }
     }
 }
-// Of a row with a teacher: all as if outside S, then those in S, by the threads that have stored them.  X: the student's logits of the entries are in
-// t.x; else they are read here, before this wave, which alone stores them, does.
-template <int NT, int G, bool X, bool BF16, int U>
+// Of a row with a teacher: all as if outside S, then those in S, from the lanes that have them as entries; xs: their logits.  (The stores of a wave to
+// one address take effect in the order of its instructions.)
+template <int NT, int G, bool BF16, int U>
 __device__ __forceinline__ void distill_put_go(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
-                                               const Raw<BF16, U> &raw) {
-    const int here = it * (NT / 64) + (threadIdx.x >> 6);
-    u64 any = 0;
-    float g[SLOTS];
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-        g[s] = 0.f;
-        if (s && a.k <= 64 * s) break;  // uniform
-        const u64 hits = ballot(E.where[s] == here);
-        any |= hits;
-        if (hits) {
-            const int i = 64 * s + lane_id();
-            Slope in = d.out;
-            in.a = d.in_s;
-            const float x = X ? t.x[i] : E.where[s] == here ? row.at(t.id[i]) : 0.f;
-            g[s] = slope_at<false>(in, x) - d.w * t.sum[i];
-        }
-    }
+                                               const Raw<BF16, U> &raw, const float (&xs)[SLOTS]) {
     put_go<NT, G, false>(row, it, d.out, a.grad, d.at, raw);
-    if (any)
-        entries_at(a, E, here, [&](int lane, int, int i) {
-            const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(i < 64 ? g[0] : g[SLOTS - 1]), i & 63));
-            if (lane_id() == lane) put_elem<BF16>(a.grad, d.at + t.id[i], v);
-        });
+    wave_sync();
+    const int here = it * (NT / 64) + (threadIdx.x >> 6);
+    Slope in = d.out;
+    in.a = d.in_s;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+        if (E.where[s] == here) {
+            const int i = 64 * s + lane_id();
+            put_elem<BF16>(a.grad, d.at + t.id[i], slope_at<false>(in, xs[s]) - d.w * t.sum[i]);
+        }
 }
 template <bool BF16>
 __device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, float x) {
@@ -351,6 +368,10 @@ __device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const R
     entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(in, x) - d.w * t.sum[i] : g; });
     if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
 }
+__device__ __forceinline__ void s_elems(const Teacher &t, float (&x)[SLOTS]) {
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) x[s] = t.x[64 * s + lane_id()];
+}
 template <bool BF16>
 __device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, float (&x)[SLOTS]) {
 #pragma unroll
@@ -359,10 +380,11 @@ __device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, fl
 
 // ---- rows that a workgroup holds: read once ----
 template <bool BF16, bool GRAD, int NT, int U>
-__global__ __launch_bounds__(NT, NT == 1024 ? 4 : BF16 ? 8 : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
+__global__ __launch_bounds__(NT, NT == 1024 ? 4 : NT == 64 ? 5 : BF16 ? 8 : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
     constexpr int G = U == 4 ? 4 : 2;  // units that are worked on at once
     __shared__ Teacher t;
     __shared__ Sums room[NT / 64];
+    __shared__ u32 marks[NT * U / 4];
     const int64_t r = blockIdx.x;
     const int64_t tr = teacher_row(a, r);
     if (tr < 0) {
@@ -385,7 +407,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : BF16 ? 8 : U == 4 ? 6 : 4) voi
         s_elems<BF16>(row, given, xs);
         teacher_probs(a, lse, given, xs, t);
     }
-    const Hidden<NT, U> hidden(a, E, 0);
+    const Hidden<NT, U> hidden(E, 0, marks);
     Sums s = {-INFINITY, 0.f, 0.f};
     bool zeros = false;
 #pragma unroll
@@ -402,7 +424,9 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : BF16 ? 8 : U == 4 ? 6 : 4) voi
     if (lead) loss_write(a, r, t, R);
     if (GRAD) {
         const DistillSlope d = {slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride};
-        distill_put_go<NT, G, true>(a, row, 0, E, t, d, raw);
+        float xs[SLOTS];
+        s_elems(t, xs);
+        distill_put_go<NT, G>(a, row, 0, E, t, d, raw, xs);
         distill_grad_loose(a, row, E, t, d, xl);
     }
 }
@@ -412,6 +436,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : BF16 ? 8 : U == 4 ? 6 : 4) voi
 template <bool BF16, bool KEEP>
 __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF16> &row, const Entries &E, int first, int end, bool loose) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
+    __shared__ u32 marks[NT * U / 4];
     Sums s = {-INFINITY, 0.f, 0.f};
     bool zeros = false;
     for (int it = first; it < end; ++it) {
@@ -419,7 +444,7 @@ __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF1
         go_request<NT, KEEP>(row, it, raw);
         float x[8 * U];
         go_take<NT, U>(row, it, raw, 0, x);
-        Hidden<NT, U>(a, E, it).template hide<U>(0, x);
+        Hidden<NT, U>(E, it, marks).template hide<U>(0, x);
         sums_add<false>(s, x, max_of(x), a.c, zeros);
     }
     if (loose && row.loose > 0) {
@@ -428,13 +453,13 @@ __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF1
     }
     return s;
 }
-template <bool X, bool BF16>
+template <bool BF16>
 __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, int first, int end,
-                                          bool loose, Raw<BF16, STREAM_U> raw) {
+                                          bool loose, Raw<BF16, STREAM_U> raw, const float (&xs)[SLOTS]) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     for (int it = first; it < end; ++it) {
         if (it > first) go_request<NT, false>(row, it, raw);
-        distill_put_go<NT, U, X>(a, row, it, E, t, d, raw);
+        distill_put_go<NT, U>(a, row, it, E, t, d, raw, xs);
     }
     if (loose) {
         const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
@@ -474,7 +499,9 @@ __global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a
     if (lead) loss_write(a, r, t, R);
     Raw<BF16, U> raw = {};
     if (GRAD && goes > 0) go_request<NT, false>(row, 0, raw);
-    if (GRAD) grad_goes<true>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true, raw);
+    float xs[SLOTS];
+    s_elems(t, xs);
+    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true, raw, xs);
 }
 
 // Sums outside S of a part of a row, and from the first part the elements of S (the next launch may write their gradients over them).
@@ -546,7 +573,9 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     else wave_sync();
     const RowLoss R = row_loss(a, w, t, out);
     if (lead && part == 0) loss_write(a, r, t, R);
-    if (GRAD) grad_goes<true>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0, raw);
+    float xs[SLOTS];
+    s_elems(t, xs);
+    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of a part of a row from what the loss has saved.
@@ -573,13 +602,17 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     Raw<BF16, U> raw = {};
     if (first < end) go_request<NT, false>(row, first, raw);
     entries_place<NT, U>(a, row, G, E);
-    if (threadIdx.x < 64) {
-        const float none[SLOTS] = {};
-        teacher_probs(a, lse, G, none, t);
+    // The logits of the entries that this wave is to store: no other stores them.
+    float xs[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int go = E.where[s] / (NT / 64), wave = E.where[s] % (NT / 64);
+        xs[s] = E.where[s] >= 0 && go >= first && go < end && wave == (int)(threadIdx.x >> 6) ? row.at(G.id[s]) : 0.f;
     }
+    if (threadIdx.x < 64) teacher_probs(a, lse, G, xs, t);
     __syncthreads();
     const float in_s = w * (t.P + t.rest), out = tail > -INFINITY ? in_s - w * t.rest * expf(-tail) : in_s;
-    grad_goes<false>(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first, end, part == 0, raw);
+    grad_goes(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.

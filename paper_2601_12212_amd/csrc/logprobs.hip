@@ -119,16 +119,26 @@ __device__ __forceinline__ void top_offer(TopRoom<NT> &r, float mine) {
     else atomicMax(&r.tm[threadIdx.x & 255], ord32(mine) >> 16);
 }
 
-// f(rank, key) for the k best of n keys, and f(rank, 0) for ranks that have none
+// f(rank, key) for the k best of n keys, and f(rank, 0) for ranks that have none.  Up to 64 keys, as there are mostly, lie in the lanes of one wave, and each is
+// handed to all of them.
 template <int NT, class F>
 __device__ __forceinline__ void ranked(const u64 *keys, int n, int k, F f) {
+    if (n <= 64) {
+        if (threadIdx.x >= 64) return;
+        const int lane = lane_id();
+        const u64 key = lane < n ? keys[lane] : 0ull;
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += readlane_u64(key, j) > key;
+        if (lane < n && rank < k) f(rank, key);
+        if (lane >= n && lane < k) f(lane, 0ull);
+        return;
+    }
     for (int i = threadIdx.x; i < n; i += NT) {
         const u64 key = keys[i];
         int rank = 0;
         for (int j = 0; j < n; ++j) rank += keys[j] > key;
         if (rank < k) f(rank, key);
     }
-    for (int i = n + (int)threadIdx.x; i < k; i += NT) f(i, 0ull);
 }
 
 // Where entry e's row starts, or -1: it has none
@@ -221,9 +231,11 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
         for (int u = 0; u < U; ++u) {
             float x[8];
             go_take<NT, 1>(row, 0, raw, u, x);
+            const float most = max_of(x);
+            if (most >= edge && most > -INFINITY)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], row.head + 8 * (u * NT + tid) + j);
+                for (int j = 0; j < 8; ++j)
+                    if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], row.head + 8 * (u * NT + tid) + j);
         }
     }
     __syncthreads();
