@@ -373,7 +373,8 @@ int dt_commit(void *stream, int batch, int n_layers, dt_dtype t, int Hkv, int D,
  * row_of is outside 0 .. rows_per_seq-1 has no row: 0, 0, (0, 0), slots (-inf, -1), and reads nothing.  Two entries may go by
  * one row.  Logits of -inf are tokens of probability 0; a row that has no other has log-probabilities -inf, entropy 0
  * and stats (-inf, -inf).  Sums are fp32, relative to the row's largest logit.
- * Workspace: dt_logprob_workspace_bytes(batch*per_seq, V) bytes.
+ * Workspace: dt_logprob_workspace_bytes(batch*per_seq, V) bytes; what suffices for a call does for one of fewer rows or a smaller
+ * vocabulary.
  * Errors: null logits or stats, logprob without tokens, per_seq > rows_per_seq without row_of, a temperature outside 1e-4 .. 1e4, k > 0 without
  * its outputs, pointers not aligned to their elements -> DT_ERR_INVALID_ARG; k > min(DT_K_MAX, V), V > DT_VOCAB_MAX or more than
  * 2^24 - 1 entries -> DT_ERR_LIMIT.
@@ -443,7 +444,8 @@ int dt_distill_rows_grad(void *stream, int64_t n_rows, const void *logits, dt_dt
  * dt_profile_enable(0) switches it off.  dt_profile_read sums, for one kernel id
  * (0 draft row chunks, 1 row merge, 2 tree, 3 attention, 4 reserved (no launch), 5 target row
  * chunks, 6 accept, 7 dt_topk_rows chunks, 8 commit, 9 policy layer 1, 10 policy head, 11 per-node target samples,
- * 12 reward, 13 token log-probabilities, 14 their join, 15 distillation loss, 16 its join, 17 gradients of rows), the elapsed milliseconds of the launches recorded
+ * 12 reward, 13 token log-probabilities, 14 distillation loss, 15 its gradient where that takes a second
+ * launch, 16 gradients of rows), the elapsed milliseconds of the launches recorded
  * since the last enable, waiting for them to finish.  Not thread-safe.
  */
 int dt_profile_enable(int max_launches);

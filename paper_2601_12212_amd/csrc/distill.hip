@@ -10,6 +10,8 @@
 // function of log q_j: one exponential an element, which is read and written once by one thread, so that a gradient may take its logits' place.
 //
 // Which elements belong to S a wave knows from its lanes: lane i holds where entries i and 64 + i lie (go, thread, element of the thread).
+#include <algorithm>
+
 #include "vocab_rows.hpp"
 
 namespace dt {
@@ -433,9 +435,9 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : NT == 64 ? 5 : BF16 ? 8 : U ==
 
 // ---- rows that are streamed ----
 // A workgroup's sums outside S over goes first .. end - 1, and the loose elements where `loose`.
-template <bool BF16, bool KEEP>
+template <bool BF16, bool KEEP, int NT>
 __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF16> &row, const Entries &E, int first, int end, bool loose) {
-    constexpr int NT = STREAM_NT, U = STREAM_U;
+    constexpr int U = STREAM_U;
     __shared__ u32 marks[NT * U / 4];
     Sums s = {-INFINITY, 0.f, 0.f};
     bool zeros = false;
@@ -453,10 +455,10 @@ __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF1
     }
     return s;
 }
-template <bool BF16>
+template <int NT, bool BF16>
 __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, int first, int end,
                                           bool loose, Raw<BF16, STREAM_U> raw, const float (&xs)[SLOTS]) {
-    constexpr int NT = STREAM_NT, U = STREAM_U;
+    constexpr int U = STREAM_U;
     for (int it = first; it < end; ++it) {
         if (it > first) go_request<NT, false>(row, it, raw);
         distill_put_go<NT, U>(a, row, it, E, t, d, raw, xs);
@@ -468,9 +470,9 @@ __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> 
 }
 
 // Whole rows, and their gradient in a second pass over the row, which the caches then hold.
-template <bool BF16, bool GRAD>
-__global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a) {
-    constexpr int NT = STREAM_NT, U = STREAM_U;
+template <bool BF16, bool GRAD, int NT>
+__global__ __launch_bounds__(NT, 8) void distill_stream_kernel(DistillArgs a) {
+    constexpr int U = STREAM_U;
     __shared__ Teacher t;
     __shared__ Sums room[NT / 64];
     const int64_t r = blockIdx.x;
@@ -483,7 +485,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a
     const bool lead = threadIdx.x < 64;
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
-    const int goes = row.template goes<STREAM_GO>();
+    const int goes = row.template goes<NT * U>();
     Given G;
     Entries E;
     entries_load(a, tr, G);
@@ -493,7 +495,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a
         s_elems<BF16>(row, G, xs);
         teacher_probs(a, lse, G, xs, t);
     }
-    Sums s = sums_outside<BF16, GRAD>(a, row, E, 0, goes, true);
+    Sums s = sums_outside<BF16, GRAD, NT>(a, row, E, 0, goes, true);
     s = block_sums<false, NT>(s, a.c, room);
     const RowLoss R = row_loss(a, w, t, s);
     if (lead) loss_write(a, r, t, R);
@@ -501,41 +503,68 @@ __global__ __launch_bounds__(STREAM_NT) void distill_stream_kernel(DistillArgs a
     if (GRAD && goes > 0) go_request<NT, false>(row, 0, raw);
     float xs[SLOTS];
     s_elems(t, xs);
-    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true, raw, xs);
+    if (GRAD) grad_goes<NT>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true, raw, xs);
 }
 
-// Sums outside S of a part of a row, and from the first part the elements of S (the next launch may write their gradients over them).
-template <bool BF16>
+// The sums of a row's parts, from float2 at `sums`, in every lane.
+__device__ __forceinline__ Sums parts_sums(u64 *sums, int parts, float c) {
+    Sums s = {-INFINITY, 0.f, 0.f};
+    if (lane_id() < parts) {
+        const u64 p = get_agent(sums + lane_id());
+        s.m = __uint_as_float((u32)p);
+        s.s = __uint_as_float((u32)(p >> 32));
+    }
+    wave_sums<false>(s, c);
+    return s;
+}
+// Sums outside S of a part of a row.  LAST: who is last of a row's says its loss.  Else distill_join_kernel does, and finds the elements of S as the first part has left
+// them, since it may write their gradients over them.
+template <bool BF16, bool LAST>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Sums room[NT / 64];
+    __shared__ Teacher t;
     const RowPart rp = row_part(a.parts);
     const int64_t r = rp.row;
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
-    if (tr < 0) return;
+    if (tr < 0) {
+        if (LAST && part == 0) row_loss_none(a, r);
+        return;
+    }
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
     Given G;
     Entries E;
     entries_load(a, tr, G);
     entries_place<NT, U>(a, row, G, E);
-    if (part == 0 && threadIdx.x < 64) {
-        float xs[SLOTS];
+    float xs[SLOTS];
+    if (!LAST && part == 0 && threadIdx.x < 64) {
         s_elems<BF16>(row, G, xs);
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s)
             if (64 * s + lane_id() < a.k) a.s_elems[r * a.k + 64 * s + lane_id()] = xs[s];
     }
-    Sums s = sums_outside<BF16, true>(a, row, E, first, min(first + a.part_goes, row.template goes<STREAM_GO>()), part == 0);
+    Sums s = sums_outside<BF16, !LAST, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<STREAM_GO>()), part == 0);
     s = block_sums<false, NT>(s, a.c, room);
-    if (threadIdx.x == 0) ((float2 *)a.ws)[r * a.parts + part] = make_float2(s.m, s.s);
+    if (threadIdx.x >= 64) return;
+    u64 *const sums = (u64 *)a.ws + r * a.parts;
+    if (threadIdx.x == 0) put_agent(sums + part, (u64)__float_as_uint(s.s) << 32 | __float_as_uint(s.m));
+    if (!LAST) return;
+    u64 *const marks = (u64 *)a.ws + a.n * a.parts + r * a.parts;
+    if (!part_arrive(marks, part, a.parts, a.tag)) return;
+    s_elems<BF16>(row, G, xs);
+    teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
+    s = parts_sums(sums, a.parts, a.c);
+    wave_sync();
+    loss_write(a, r, t, row_loss(a, 0.f, t, s));
+    parts_leave(marks, a.parts);
 }
-// The loss of rows whose parts are there, and with GRAD the gradient of a part.
-template <bool BF16, bool GRAD>
+// The loss of rows whose parts are there, and the gradient of a part.
+template <bool BF16>
 __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
-    const RowPart rp = row_part(GRAD ? a.parts : 1);
+    const RowPart rp = row_part(a.parts);
     const int64_t r = rp.row;
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
@@ -544,38 +573,29 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     if (tr < 0) {
         if (part == 0) row_loss_none(a, r);
         const int from = min(part * a.part_goes * STREAM_ELEMS, a.V), to = min((part + 1) * a.part_goes * STREAM_ELEMS, a.V);
-        if (GRAD) grad_zero<BF16>(a.grad, r * a.grad_stride + from, to - from, NT);
+        grad_zero<BF16>(a.grad, r * a.grad_stride + from, to - from, NT);
         return;
     }
     const bool lead = threadIdx.x < 64;
-    if (!GRAD && !lead) return;
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
-    Sums out = {-INFINITY, 0.f, 0.f};
-    if (lane_id() < a.parts) {
-        const float2 p = ((const float2 *)a.ws)[r * a.parts + lane_id()];
-        out.m = p.x;
-        out.s = p.y;
-    }
     Given G;
     Entries E;
     entries_load(a, tr, G);
-    Raw<BF16, U> raw = {};
-    if (GRAD && first < end) go_request<NT, false>(row, first, raw);
-    entries_place<NT, U>(a, row, G, E);
-    wave_sums<false>(out, a.c);
+    float xs[SLOTS];
     if (lead) {
-        float xs[SLOTS];
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) xs[s] = G.id[s] >= 0 ? a.s_elems[r * a.k + 64 * s + lane_id()] : -INFINITY;
-        teacher_probs(a, lse, G, xs, t);
+        for (int s = 0; s < SLOTS; ++s) xs[s] = 64 * s + lane_id() < a.k ? a.s_elems[r * a.k + 64 * s + lane_id()] : -INFINITY;
     }
-    if (GRAD) __syncthreads();
-    else wave_sync();
+    Raw<BF16, U> raw = {};
+    if (first < end) go_request<NT, false>(row, first, raw);
+    entries_place<NT, U>(a, row, G, E);
+    const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
+    if (lead) teacher_probs(a, lse, G, xs, t);
+    __syncthreads();
     const RowLoss R = row_loss(a, w, t, out);
     if (lead && part == 0) loss_write(a, r, t, R);
-    float xs[SLOTS];
     s_elems(t, xs);
-    if (GRAD) grad_goes(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
+    grad_goes<NT>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of a part of a row from what the loss has saved.
@@ -612,7 +632,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     if (threadIdx.x < 64) teacher_probs(a, lse, G, xs, t);
     __syncthreads();
     const float in_s = w * (t.P + t.rest), out = tail > -INFINITY ? in_s - w * t.rest * expf(-tail) : in_s;
-    grad_goes(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
+    grad_goes<NT>(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.
@@ -649,53 +669,67 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
     }
 }
 
+// How rows are cut whose gradient is asked for too.  Rows of up to 131,072 bf16 entries, or half as many of fp32, fit the registers of a compute unit, a workgroup of 1,024
+// threads, which then reads them once; while it waits, though, the compute unit has nothing else.  So: with one row to a compute unit, or many, and long ones.
+// Loss and gradient, us, in parts | held | whole (read twice, the second time from the caches), bf16:
+//     V = 50,001:  n = 64 12.4 | 12.2 | 15.9;  200 16.8 | 12.9 | 18.0;  300 21.7 | 24.2 | 22.1;  800 48 | 49 | 43;  2,048 100 | 101 | 100
+//     V = 128,256: n = 64 13.7 | 20.0 | 30.4;  200 27.2 | 23.5 | 35.5;  300 40.4 | 43.8 | 44.2;  800 102 | 94 | 100;  2,048 246 | 198 | 246
+static Cut grad_cut(int64_t n, int V, bool bf16) {
+    const Cut c = rows_cut(n, V, bf16);
+    if (c == HELD || c == PARTS || V < HELD_LEAST) return c;
+    const bool fits = V <= (bf16 ? 131072 : 65536), is_long = (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024;
+    if (fits && (n <= CUS || (is_long && n >= 3 * CUS / 2))) return HELD;
+    return n < 3 * CUS / 2 ? PARTS : WHOLE;
+}
 template <bool BF16, bool GRAD>
 static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
     const auto held = [&](auto h) {
         constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
         launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
     };
-    if (rows_held(a.V)) {
+    const Cut cut = GRAD ? grad_cut(a.n, a.V, BF16) : rows_cut(a.n, a.V, BF16);
+    if (cut == HELD && a.V <= HELD_V) {
         by_held(a.V, held);
-        return hipGetLastError();
-    }
-    if constexpr (GRAD)
-        if (rows_held_long(a.n, a.V, BF16)) {
+    } else if (cut == HELD) {
+        if constexpr (GRAD) {
             if (a.V <= 65536) held(Held<1024, 8>());
             else if constexpr (BF16) held(Held<1024, 16>());
-            return hipGetLastError();
         }
-    if (a.parts == 1) {
-        launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, GRAD>, dim3((u32)a.n), dim3(STREAM_NT), 0, a);
-        return hipGetLastError();
+    } else if (cut == PARTS) {
+        launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, !GRAD>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || !GRAD) return e;
+        launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
+    } else if (cut == WIDE) {
+        if constexpr (!GRAD) launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, false, WIDE_NT>, dim3((u32)a.n), dim3(WIDE_NT), 0, a);
+    } else {
+        launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, GRAD, STREAM_NT>, dim3((u32)a.n), dim3(STREAM_NT), 0, a);
     }
-    launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16, GRAD>, dim3((u32)(GRAD ? a.n * a.parts : a.n)), dim3(STREAM_NT), 0, a);
     return hipGetLastError();
 }
 
+// Sums of the parts, then their marks or, with the gradient, the elements of S: as many as parts can be, as for logprob_workspace.
 size_t distill_workspace(int64_t n, int V) {
-    const int parts = row_parts(V, part_goes(n, V));
-    if (rows_held(V) || parts == 1) return 0;
-    return (size_t)n * (parts * sizeof(float2) + DT_DISTILL_K_MAX * sizeof(float));
+    const size_t goes = row_goes(V);
+    return (size_t)std::min(n, 3 * CUS / 2 - 1) * (goes * 8 + std::max<size_t>(goes * 8, DT_DISTILL_K_MAX * sizeof(float)));
 }
 hipError_t distill_launch(DistillArgs a, hipStream_t st) {
     a.part_goes = part_goes(a.n, a.V);
     a.parts = row_parts(a.V, a.part_goes);
-    a.s_elems = (float *)((float2 *)a.ws + a.n * a.parts);
+    a.s_elems = (float *)((u64 *)a.ws + a.n * a.parts);
+    a.tag = launch_tag();
     if (a.dtype == DT_BF16) return a.grad ? launch_distill<true, true>(a, st) : launch_distill<true, false>(a, st);
     return a.grad ? launch_distill<false, true>(a, st) : launch_distill<false, false>(a, st);
 }
-// goes of a part where nothing joins the parts: a launch has up to 2^32 - 1 threads
-static int grad_goes_of(int64_t n, int V, int least) {
-    int per = least;
+// Goes of a part where nothing joins the parts: one, unless that took more than the 2^32 - 1 threads of a launch.  (Workgroups that start together
+// then read and write side by side: 8,192 rows of 32,000 bf16 entries 179 us, with two goes 194, four, whole rows, 198; a copy of as many bytes 167 and 190.)
+static int grad_goes_of(int64_t n, int V) {
+    int per = 1;
     while (n * row_parts(V, per) > ((int64_t)1 << 24) - 1) ++per;
     return per;
 }
 hipError_t distill_grad_launch(DistillArgs a, hipStream_t st) {
-    a.part_goes = grad_goes_of(a.n, a.V, (int)tune("DT_DG", 1));
+    a.part_goes = grad_goes_of(a.n, a.V);
     a.parts = row_parts(a.V, a.part_goes);
     const dim3 grid((u32)(a.n * a.parts));
     if (a.dtype == DT_BF16) launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<true>, grid, dim3(STREAM_NT), 0, a);
@@ -709,7 +743,7 @@ static void launch_logprob_grad(const LogprobGradArgs &a, hipStream_t st) {
     else launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
 }
 hipError_t logprob_grad_launch(LogprobGradArgs a, hipStream_t st) {
-    a.part_goes = grad_goes_of(a.n, a.V, (int)tune("DT_LG", 1));
+    a.part_goes = grad_goes_of(a.n, a.V);
     a.parts = row_parts(a.V, a.part_goes);
     if (a.dtype == DT_BF16) launch_logprob_grad<true>(a, st);
     else launch_logprob_grad<false>(a, st);

@@ -16,7 +16,7 @@ namespace dt {
 // kernel's own begin and end; dt_profile_read sums the elapsed times per kernel id.
 enum KernelId { KID_ROWS_DRAFT = 0, KID_ROWS_MERGE, KID_TREE, KID_ATTN, KID_RESERVED_4 /* no launch; the others keep their numbers */, KID_ROWS_TARGET,
                 KID_ACCEPT, KID_ROWS_UNIFORM, KID_COMMIT, KID_POLICY_L1, KID_POLICY_HEAD, KID_NODE_SAMPLE, KID_REWARD,
-                KID_LOGPROBS, KID_LOGPROBS_JOIN, KID_DISTILL, KID_DISTILL_JOIN, KID_ROWS_GRAD, KID_COUNT };
+                KID_LOGPROBS, KID_DISTILL, KID_DISTILL_JOIN, KID_ROWS_GRAD, KID_COUNT };
 bool prof_next(int kid, hipEvent_t *start, hipEvent_t *stop);  // false when timing is off
 
 template <typename F, typename... Args>
@@ -204,9 +204,11 @@ struct LogprobArgs {
     float *logprob, *entropy, *stats;     // the first two may be null
     float *top_logprob;                   // [n, k]
     int32_t *top_id;
-    void *ws;                             // sums of the parts of rows, then
-    uint16_t *slots;                      // [n, goes, 256] the largest of every thread's elements of a go, upper halves of ordered images
-    int goes, parts, part_goes;           // set by the launch
+    void *ws;                             // [n, parts] sums of the parts of rows, then
+    unsigned long long *marks;            // [n, parts], and
+    unsigned long long *slots;            // [n, goes, 64] the largest of every thread's elements of a go, upper halves of ordered images
+    unsigned long long tag;               // of the launch; these and the next are set by it
+    int goes, parts, part_goes;
 };
 size_t logprob_workspace(int64_t n, int V);
 hipError_t logprob_launch(LogprobArgs a, hipStream_t st);
@@ -236,7 +238,8 @@ struct DistillArgs {
     void *grad;                              // or null
     void *ws;                                // sums of the parts of rows, then
     float *s_elems;                          // [n, k] the student's logits of the teacher's tokens
-    int parts, part_goes;                    // set by the launch
+    unsigned long long tag;                  // of the launch; this and the next are set by it
+    int parts, part_goes;
 };
 size_t distill_workspace(int64_t n, int V);
 hipError_t distill_launch(DistillArgs a, hipStream_t st);

@@ -8,6 +8,8 @@
 // 32 elements of a go as such a key, a `slot`; the few slots that reach the bound are read again, their elements that reach it listed, and the list
 // ranked by counting keys of (value, id).  A list that overflows (ties, a row whose best are neighbours) gives way to a radix selection over
 // the row, eight bits at a time, and the ties that still fit are taken in ascending id.
+#include <algorithm>
+
 #include "vocab_rows.hpp"
 
 namespace dt {
@@ -248,27 +250,23 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
 }
 
 // ---- rows that are streamed ----
-struct Part {  // of a row, left for logprob_join_kernel
-    float m, s, w, pad;
-};
-extern __shared__ __align__(16) unsigned char lp_lds[];
-
-// The candidates among the slots that reach the bound: slot i of the row is go i / NT, thread i % NT.  Ends with a barrier; the number found.
-template <int NT, bool BF16, class Slot>
-__device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row, int k, float mine, Slot slot) {
+// A slot is the largest of a thread's elements of a go, the upper half of its ordered image: slot i of the row is that of go i / NT, thread i % NT.  Found by
+// top_of_slots: the candidates among the slots that reach the bound.  each(f): f(slot, key) for some of the slots, all in all by the threads; mine: the largest key of a thread's.
+// Ends with a barrier; the number found.
+template <int NT, bool BF16, class Each>
+__device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row, int k, u32 mine, Each each) {
     constexpr int U = STREAM_U;
     typedef TopRoom<NT> R;
-    const int tid = threadIdx.x, goes = row.template goes<NT * U>();
-    const u32 kth = top_bound<NT>(r, mine, k);
+    const int tid = threadIdx.x;
+    const u32 kth = top_bound<NT>(r, 0.f, k);
     const float edge = key_edge(kth);
-    if (r.tm[tid & 255] >= kth)
-        for (int it = 0; it < goes; ++it) {
-            const u32 key = slot(it);
+    if (mine >= kth)
+        each([&](int slot, u32 key) {
             if (key >= kth && key > NO_KEY) {
                 const u32 at = atomicAdd(&r.hits, 1u);
-                if (at < R::HITS) r.hit[at] = (u32)(it * NT + tid);
+                if (at < R::HITS) r.hit[at] = (u32)slot;
             }
-        }
+        });
     if (tid < row.loose) {
         const int i = row.loose_at(tid);
         const float x = row.at(i);
@@ -304,24 +302,25 @@ __device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row
     return (int)r.n;
 }
 
-// Goes of a row, from part * part_goes on: all of them (JOIN false) or a part's, for logprob_join_kernel.
-template <bool BF16, bool ENT, bool TOP, bool JOIN, int NT>
+extern __shared__ __align__(16) unsigned char lp_lds[];
+
+// Whole rows.
+template <bool BF16, bool ENT, bool TOP, int NT>
 __global__ __launch_bounds__(NT, 8) void logprob_stream_kernel(LogprobArgs a) {
     constexpr int U = STREAM_U;
-    const RowPart rp = row_part(JOIN ? a.parts : 1);
-    const int64_t e = rp.row;
-    const int part = rp.part, tid = threadIdx.x;
+    const int64_t e = blockIdx.x;
+    const int tid = threadIdx.x;
     __shared__ Sums s_sums[NT / 64];
-    TopRoom<NT> &room = *(TopRoom<NT> *)lp_lds;  // TOP && !JOIN, and behind it the slots
-    uint16_t *const slots = JOIN ? a.slots + (e * a.goes) * NT + tid : (uint16_t *)(&room + 1) + tid;
+    TopRoom<NT> &room = *(TopRoom<NT> *)lp_lds;  // TOP, and behind it the slots
+    uint16_t *const slots = (uint16_t *)(&room + 1) + tid;
     const int64_t at = entry_row(a, e);
     if (at < 0) {
-        if (!JOIN) entry_none(a, e);
+        entry_none(a, e);
         return;
     }
     const Row<BF16> row(a.logits, at, a.V);
-    const float xy = JOIN ? 0.f : token_logit<BF16>(a, e, at);
-    if (TOP && !JOIN) {
+    const float xy = token_logit<BF16>(a, e, at);
+    if (TOP) {
         if (tid == 0) room.n = room.hits = 0;
         if (NT > 256) {
             if (tid < 256) room.tm[tid] = NO_KEY;
@@ -330,10 +329,9 @@ __global__ __launch_bounds__(NT, 8) void logprob_stream_kernel(LogprobArgs a) {
     }
     Sums r = {-INFINITY, 0.f, 0.f};
     float mine = -INFINITY;
-    const int end = JOIN ? min((part + 1) * a.part_goes, row.template goes<NT * U>()) : row.template goes<NT * U>();
+    const int goes = row.template goes<NT * U>();
     bool zeros = false;
-    int it = JOIN ? part * a.part_goes : 0;
-    for (; it < end; ++it) {
+    for (int it = 0; it < goes; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, false>(row, it, raw);
         float x[8 * U];
@@ -345,87 +343,130 @@ __global__ __launch_bounds__(NT, 8) void logprob_stream_kernel(LogprobArgs a) {
         }
         sums_add<ENT>(r, x, mx, a.c, zeros);
     }
-    if (part == 0 && tid < row.loose) sums_add1<ENT>(r, row.at(row.loose_at(tid)), a.c);
-    if (TOP && !JOIN) top_offer<NT>(room, mine);
+    if (tid < row.loose) sums_add1<ENT>(r, row.at(row.loose_at(tid)), a.c);
+    if (TOP) top_offer<NT>(room, mine);
     r = block_sums<ENT, NT>(r, a.c, s_sums);
-    if (JOIN) {
-        if (tid == 0) ((Part *)a.ws)[e * a.parts + part] = Part{r.m, r.s, r.w, 0.f};
-        return;
-    }
-    const RowStat st = row_stat(r.m, r.s, a.c);
-    if (tid == NT - 1) entry_write(a, e, xy, r, st);
-    if (TOP) {
-        const int found = top_of_slots<NT, BF16>(room, row, a.k, mine, [&](int it) { return (u32)slots[it * NT]; });
-        alternatives_write<NT>(a, e, room, found, st);
-    }
-}
-
-// The parts of a row together.
-template <bool BF16, bool TOP>
-__global__ __launch_bounds__(STREAM_NT, 4) void logprob_join_kernel(LogprobArgs a) {
-    constexpr int NT = STREAM_NT;
-    const int64_t e = blockIdx.x;
-    const int tid = threadIdx.x;
-    TopRoom<NT> &room = *(TopRoom<NT> *)lp_lds;  // TOP, and behind it the slots
-    uint16_t *const slots = (uint16_t *)(&room + 1);
-    const int64_t at = entry_row(a, e);
-    if (at < 0) {
-        entry_none(a, e);
-        return;
-    }
-    const Row<BF16> row(a.logits, at, a.V);
-    const float xy = token_logit<BF16>(a, e, at);
-    Sums r = {-INFINITY, 0.f, 0.f};
-    if (lane_id() < a.parts) {
-        const Part p = ((const Part *)a.ws)[e * a.parts + lane_id()];
-        r = Sums{p.m, p.s, p.w};
-    }
-    const int goes = row.template goes<STREAM_GO>();
-    if (TOP) {
-        if (tid == 0) room.n = room.hits = 0;
-        constexpr int MOST = (DT_VOCAB_MAX / STREAM_ELEMS * NT * 2 / 16 + NT - 1) / NT;
-        const Vec16 *const from = (const Vec16 *)(a.slots + e * a.goes * NT);
-        Vec16 v[MOST];
-#pragma unroll
-        for (int i = 0; i < MOST; ++i)
-            if (i * NT + tid < goes * NT / 8) v[i] = from[i * NT + tid];
-#pragma unroll
-        for (int i = 0; i < MOST; ++i)
-            if (i * NT + tid < goes * NT / 8) ((Vec16 *)slots)[i * NT + tid] = v[i];
-    }
-    wave_sums<true>(r, a.c);
     const RowStat st = row_stat(r.m, r.s, a.c);
     if (tid == NT - 1) entry_write(a, e, xy, r, st);
     if (!TOP) return;
-    __syncthreads();
+    const int found = top_of_slots<NT>(room, row, a.k, ord32(mine) >> 16, [&](auto f) {
+        for (int it = 0; it < goes; ++it) f(it * NT + tid, (u32)slots[it * NT]);
+    });
+    alternatives_write<NT>(a, e, room, found, st);
+}
+
+// Parts of a row, part_goes goes each.  The slots go to the memory side four to a word.
+template <bool BF16, bool ENT, bool TOP>
+__global__ __launch_bounds__(STREAM_NT, 8) void logprob_parts_kernel(LogprobArgs a) {
+    constexpr int NT = STREAM_NT, U = STREAM_U, WORDS = NT / 4;  // words of a go
+    const RowPart rp = row_part(a.parts);
+    const int64_t e = rp.row;
+    const int part = rp.part, tid = threadIdx.x;
+    __shared__ Sums s_sums[NT / 64];
+    __shared__ TopRoom<TOP ? NT : 64> room_;
+    __shared__ bool s_last;
+    TopRoom<NT> &room = (TopRoom<NT> &)room_;
+    const int64_t at = entry_row(a, e);
+    if (at < 0) {
+        if (part == 0) entry_none(a, e);
+        return;
+    }
+    const Row<BF16> row(a.logits, at, a.V);
+    u64 *const slots = a.slots + e * a.goes * WORDS;
+    Sums r = {-INFINITY, 0.f, 0.f};
+    const int goes = row.template goes<STREAM_GO>(), end = min((part + 1) * a.part_goes, goes);
+    bool zeros = false;
+    for (int it = part * a.part_goes; it < end; ++it) {
+        Raw<BF16, U> raw;
+        go_request<NT, false>(row, it, raw);
+        float x[8 * U];
+        go_take<NT, U>(row, it, raw, 0, x);
+        const float mx = max_of(x);
+        if (TOP) {
+            const int key = (int)(ord32(mx) >> 16);
+            const u32 lo = (u32)dpp_mov<0x00, 0xf>(0, key) | (u32)dpp_mov<0x55, 0xf>(0, key) << 16;  // those of a quad
+            const u32 hi = (u32)dpp_mov<0xAA, 0xf>(0, key) | (u32)dpp_mov<0xFF, 0xf>(0, key) << 16;
+            if ((tid & 3) == 0) put_agent(slots + it * WORDS + tid / 4, (u64)hi << 32 | lo);
+        }
+        sums_add<ENT>(r, x, mx, a.c, zeros);
+    }
+    if (part == 0 && tid < row.loose) sums_add1<ENT>(r, row.at(row.loose_at(tid)), a.c);
+    if (TOP) {
+        if (tid == 0) room.n = room.hits = 0;
+        drain();  // the slots are there before the barrier, and the first wave's mark comes behind it
+    }
+    r = block_sums<ENT, NT>(r, a.c, s_sums);
+    u64 *const sums = (u64 *)a.ws + 2 * e * a.parts, *const marks = a.marks + e * a.parts;
+    if (tid < 64) {
+        if (tid == 0) {
+            put_agent(sums + 2 * part, (u64)__float_as_uint(r.s) << 32 | __float_as_uint(r.m));
+            put_agent(sums + 2 * part + 1, (u64)__float_as_uint(r.w));
+        }
+        const bool last = part_arrive(marks, part, a.parts, a.tag);
+        if (TOP && tid == 0) s_last = last;
+        if (!TOP && !last) return;
+    } else if (!TOP)
+        return;
+    if (TOP) {
+        __syncthreads();
+        if (!s_last) return;
+    }
+    // The parts of the row together.
+    const float xy = token_logit<BF16>(a, e, at);
+    u64 word[4], lo = 0, hi = 0;  // of slots, the first 1,024 of the row's
+    const int words = goes * WORDS;
+    if (TOP) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) word[i] = get_agent(slots + min(i * NT + tid, words - 1));
+    }
+    r = Sums{-INFINITY, 0.f, 0.f};
+    if (lane_id() < a.parts) {
+        lo = get_agent(sums + 2 * lane_id());
+        hi = get_agent(sums + 2 * lane_id() + 1);
+        r = Sums{__uint_as_float((u32)lo), __uint_as_float((u32)(lo >> 32)), __uint_as_float((u32)hi)};
+    }
+    wave_sums<ENT>(r, a.c);
+    const RowStat st = row_stat(r.m, r.s, a.c);
+    if (tid == 0) entry_write(a, e, xy, r, st);
+    if (tid < 64) parts_leave(marks, a.parts);
+    if (!TOP) return;
+    const auto each = [&](auto f) {
+        const auto four = [&](int at, u64 w) {
+            if (at < words)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f(4 * at + j, (u32)(w >> 16 * j) & 0xFFFFu);
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) four(i * NT + tid, word[i]);
+        for (int at = 4 * NT + tid; at < words; at += NT) four(at, get_agent(slots + at));
+    };
     u32 best = NO_KEY;
-    for (int it = 0; it < goes; ++it) best = max(best, (u32)slots[it * NT + tid]);
+    each([&](int, u32 key) { best = max(best, key); });
     room.tm[tid] = best;
     __syncthreads();
-    const int found = top_of_slots<NT, BF16>(room, row, a.k, 0.f, [&](int it) { return (u32)slots[it * NT + tid]; });
+    const int found = top_of_slots<NT>(room, row, a.k, best, each);
     alternatives_write<NT>(a, e, room, found, st);
 }
 
 template <bool BF16, bool ENT, bool TOP>
 static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
-    if (rows_held(a.V)) {
-        by_held(a.V, [&](auto h) {
-            constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
-            launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
-        });
-        return hipGetLastError();
-    }
-    const size_t lds = TOP ? sizeof(TopRoom<STREAM_NT>) + (size_t)a.goes * STREAM_NT * 2 : 0;
-    if (a.parts == 1) {
-        const size_t lds4 = TOP ? sizeof(TopRoom<1024>) + (size_t)((a.V + 32767) / 32768) * 2048 : 0, lds2 = TOP ? sizeof(TopRoom<512>) + (size_t)((a.V + 16383) / 16384) * 1024 : 0;
-        if (long_nt() == 256) launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false, 256>, dim3((u32)a.n), dim3(256), lds, a);
-        else if (long_nt() == 512) launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false, 512>, dim3((u32)a.n), dim3(512), lds2, a);
-        else launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, false, 1024>, dim3((u32)a.n), dim3(1024), lds4, a);
-    } else {
-        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, true, STREAM_NT>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        launch_kernel(KID_LOGPROBS_JOIN, st, logprob_join_kernel<BF16, TOP>, dim3((u32)a.n), dim3(STREAM_NT), lds, a);
+    const auto whole = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        const size_t goes = (a.V + NT * STREAM_U * 8 - 1) / (NT * STREAM_U * 8), lds = TOP ? sizeof(TopRoom<NT>) + goes * NT * 2 : 0;
+        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, NT>, dim3((u32)a.n), dim3(NT), lds, a);
+    };
+    switch (rows_cut(a.n, a.V, BF16)) {
+        case HELD:
+            by_held(a.V, [&](auto h) {
+                constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
+                launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
+            });
+            break;
+        case PARTS:
+            launch_kernel(KID_LOGPROBS, st, logprob_parts_kernel<BF16, ENT, TOP>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
+            break;
+        case WIDE: whole(std::integral_constant<int, WIDE_NT>()); break;
+        case WHOLE: whole(std::integral_constant<int, STREAM_NT>()); break;
     }
     return hipGetLastError();
 }
@@ -435,16 +476,15 @@ static hipError_t launch_type(const LogprobArgs &a, hipStream_t st) {
     return a.k ? launch_rows<BF16, false, true>(a, st) : launch_rows<BF16, false, false>(a, st);
 }
 
-size_t logprob_workspace(int64_t n, int V) {
-    const int parts = row_parts(V, part_goes(n, V));
-    if (rows_held(V) || parts == 1) return 0;
-    return (size_t)n * parts * sizeof(Part) + (size_t)n * row_goes(V) * STREAM_NT * 2;
-}
+// Sums of the parts, their marks, slots: as many as parts can be, so that what suffices for a call does for one of fewer or shorter rows.
+size_t logprob_workspace(int64_t n, int V) { return (size_t)std::min(n, PARTS_ROWS - 1) * row_goes(V) * (24 + STREAM_NT * 2); }
 hipError_t logprob_launch(LogprobArgs a, hipStream_t st) {
     a.goes = row_goes(a.V);
     a.part_goes = part_goes(a.n, a.V);
     a.parts = row_parts(a.V, a.part_goes);
-    a.slots = (uint16_t *)((Part *)a.ws + a.n * a.parts);
+    a.marks = (u64 *)a.ws + 2 * a.n * a.parts;
+    a.slots = a.marks + a.n * a.parts;
+    a.tag = launch_tag();
     return a.dtype == DT_BF16 ? launch_type<true>(a, st) : launch_type<false>(a, st);
 }
 

@@ -9,7 +9,6 @@
 // Where that rounding is itself a large power (|m c| from 2^20 on, up to rows that hold nothing but masks of the type's lowest value)
 // the exponent is (x - m) c.
 #pragma once
-#include <cstdlib>
 #include <type_traits>
 
 #include "common.hpp"
@@ -253,19 +252,60 @@ __device__ __forceinline__ float log_prob(float x, const RowStat &r, float c) {
     return r.m == -INFINITY ? -INFINITY : (log2_weight(x, r.m, c) - r.log2s) * LN2;
 }
 
+// ---- parts of a row that meet in their own launch ----------------------------------------------------
+// Every part leaves what it has at the memory side, then a mark, the launch's number; who then sees the marks of all parts joins them.  The part whose mark
+// lands last sees them all; the one before it may as well, and does the same over again.  Nobody waits.  Marks are taken away by who has joined, for a replayed
+// graph, whose launches have the same number.
+// By one wave, behind what it has left there.  True: all are there.
+__device__ __forceinline__ bool part_arrive(u64 *marks, int part, int parts, u64 tag) {
+    drain();
+    if (lane_id() == 0) put_agent(marks + part, tag);
+    drain();
+    return ballot(lane_id() < parts && get_agent(marks + min(lane_id(), parts - 1)) != tag) == 0ull;
+}
+__device__ __forceinline__ void parts_leave(u64 *marks, int parts) {
+    if (lane_id() < parts) put_agent(marks + lane_id(), 0);
+}
+
 // ---- how a call of n rows is cut -------------------------------------------------------------------
-// Rows that one workgroup holds in its registers are read once and take one launch.  Longer ones are streamed, whole rows to a
-// workgroup where there are enough to fill the chip (STREAM_ROWS), else parts of a row, of a go at least, that a second launch joins.
-inline int64_t tune(const char *n, int64_t d) { const char *e = getenv(n); return e ? atoll(e) : d; }
-inline int long_nt() { static int64_t v = tune("DT_NT", 256); return (int)v; }
-constexpr int STREAM_NT = 256, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
-inline int64_t stream_rows() { static int64_t v = tune("DT_SR", 2048); return v; }
-inline int64_t stream_wgs() { static int64_t v = tune("DT_WG", 2048); return v; }
+// A go of a workgroup that streams reads 8,192 elements, 16 or 32 KB; with four times the threads, four times that.
+constexpr int STREAM_NT = 256, WIDE_NT = 1024, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
 inline int row_goes(int V) { return (V + STREAM_ELEMS - 1) / STREAM_ELEMS; }
-// goes of a part; parts of a row (up to 64)
+// Workgroups that hold a row in their registers: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries.
+template <int NT_, int U_>
+struct Held {
+    static constexpr int NT = NT_, U = U_;
+};
+template <class F>
+inline void by_held(int V, F f) {
+    if (V <= 2048) f(Held<64, 4>());
+    else if (V <= 8192) f(Held<256, 4>());
+    else if (V <= 16384) f(Held<256, 8>());
+    else f(Held<512, 8>());
+}
+constexpr int HELD_LEAST = 32, HELD_V = 32768;  // (shorter rows may have no whole unit)
+enum Cut {
+    HELD,   // a workgroup holds a row: one launch, read once, whatever the number of rows
+    PARTS,  // a row is many workgroups', which meet
+    WIDE,   // whole rows, 1,024 threads to each
+    WHOLE   // whole rows, 256 threads to each
+};
+// Rows that are streamed: few are cut, so that they fill the chip; while there is one to a compute unit, or up to eight of 160 KB and more, its
+// reading is what takes the time, and 1,024 threads read it; else rows are there by the thousand, and eight small workgroups to a compute unit overlap one's
+// end with another's reading.  Log-probabilities of n rows of V bf16 entries, us, with no / 20 alternatives, in parts | wide | whole:
+//     V = 50,001:  n = 64 7.3 / 11.6 | 9.1 / 12.4 | 10.8 / 15.1;  200 9.5 / 15.8 | 9.8 / 13.1 | 11.6 / 15.5;  500 14.4 / 22.5 | 15.9 / 19.1 | 13.9 / 18.1
+//     V = 128,256: n = 64 8.8 / 14.1 | 12.1 / 15.8 | 20.4 / 25.2;  200 15.0 / 22.8 | 13.3 / 16.6 | 21.7 / 26.4;  1,200 55.7 / 74.2 | 53.0 / 60.1 | 54.1 / 59.9
+constexpr int64_t PARTS_ROWS = 128, CUS = 256, MANY_ROWS = 2048;
+inline Cut rows_cut(int64_t n, int V, bool bf16) {
+    if (V >= HELD_LEAST && V <= HELD_V) return HELD;
+    if (V < HELD_LEAST) return WHOLE;
+    if (n < PARTS_ROWS) return PARTS;
+    return n <= CUS || (n < MANY_ROWS && (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024) ? WIDE : WHOLE;
+}
+// goes of a part, so that there are about eight workgroups to a compute unit; parts of a row (up to 64)
 inline int part_goes(int64_t n, int V) {
     const int goes = row_goes(V);
-    const int64_t parts = n < stream_rows() ? (stream_wgs() + n - 1) / (n > 0 ? n : 1) : 1;
+    const int64_t parts = (8 * CUS + n - 1) / n;
     return parts >= goes ? 1 : (int)((goes + parts - 1) / parts);
 }
 inline int row_parts(int V, int part_goes) { return (row_goes(V) + part_goes - 1) / part_goes; }
@@ -278,22 +318,5 @@ __device__ __forceinline__ RowPart row_part(int parts) {
     const u32 r = parts == 1 ? blockIdx.x : blockIdx.x / (u32)parts;
     return RowPart{(int64_t)r, (int)(blockIdx.x - r * (u32)parts)};
 }
-// Workgroups that hold a row: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries, false if none does.
-template <int NT_, int U_>
-struct Held {
-    static constexpr int NT = NT_, U = U_;
-};
-template <class F>
-inline void by_held(int V, F f) {
-    if (V <= 2048) f(Held<64, 4>());
-    else if (V <= 8192) f(Held<256, 4>());
-    else if (V <= 16384) f(Held<256, 8>());
-    else f(Held<512, 8>());
-}
-constexpr int HELD_V = 32768, HELD_LEAST = 32;  // (shorter ones may have no whole unit)
-inline bool rows_held(int V) { return V >= HELD_LEAST && V <= HELD_V; }
-// Longer ones, where a gradient would read them again: up to 131,072 bf16 entries, 65,536 of fp32, in the registers of a whole compute unit.
-inline int64_t held_rows() { static int64_t v = tune("DT_HR", 512); return v; }
-inline bool rows_held_long(int64_t n, int V, bool bf16) { return n >= held_rows() && V <= (bf16 ? 131072 : 65536); }
 
 }  // namespace dt
