@@ -471,7 +471,7 @@ __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> 
 
 // Whole rows, and their gradient in a second pass over the row, which the caches then hold.
 template <bool BF16, bool GRAD, int NT>
-__global__ __launch_bounds__(NT, 8) void distill_stream_kernel(DistillArgs a) {
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(DistillArgs a) {
     constexpr int U = STREAM_U;
     __shared__ Teacher t;
     __shared__ Sums room[NT / 64];
@@ -517,7 +517,7 @@ __device__ __forceinline__ Sums parts_sums(u64 *sums, int parts, float c) {
     wave_sums<false>(s, c);
     return s;
 }
-// Sums outside S of a part of a row.  LAST: who is last of a row's says its loss.  Else distill_join_kernel does, and finds the elements of S as the first part has left
+// Sums outside S of a part of a row.  LAST: who is last of a row's says its loss.  Else the next launch does, and finds the elements of S as the first part has left
 // them, since it may write their gradients over them.
 template <bool BF16, bool LAST>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
@@ -558,6 +558,29 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
     wave_sync();
     loss_write(a, r, t, row_loss(a, 0.f, t, s));
     parts_leave(marks, a.parts);
+}
+// The loss of rows whose parts are there.
+__global__ __launch_bounds__(64) void distill_loss_kernel(DistillArgs a) {
+    __shared__ Teacher t;
+    const int64_t r = blockIdx.x;
+    const int64_t tr = teacher_row(a, r);
+    if (tr < 0) {
+        row_loss_none(a, r);
+        return;
+    }
+    Given G;
+    entries_load(a, tr, G);
+    float xs[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int i = 64 * s + lane_id();
+        xs[s] = i < a.k ? a.s_elems[r * a.k + i] : -INFINITY;
+        if (!(G.id[s] >= 0 && G.id[s] < a.V && G.val[s] > -INFINITY)) G.id[s] = -1;
+    }
+    const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
+    teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
+    wave_sync();
+    loss_write(a, r, t, row_loss(a, 0.f, t, out));
 }
 // The loss of rows whose parts are there, and the gradient of a part.
 template <bool BF16>
@@ -669,17 +692,24 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
     }
 }
 
+constexpr int64_t MEET_ROWS = 3 * CUS / 2;
 // How rows are cut whose gradient is asked for too.  Rows of up to 131,072 bf16 entries, or half as many of fp32, fit the registers of a compute unit, a workgroup of 1,024
 // threads, which then reads them once; while it waits, though, the compute unit has nothing else.  So: with one row to a compute unit, or many, and long ones.
 // Loss and gradient, us, in parts | held | whole (read twice, the second time from the caches), bf16:
 //     V = 50,001:  n = 64 12.4 | 12.2 | 15.9;  200 16.8 | 12.9 | 18.0;  300 21.7 | 24.2 | 22.1;  800 48 | 49 | 43;  2,048 100 | 101 | 100
 //     V = 128,256: n = 64 13.7 | 20.0 | 30.4;  200 27.2 | 23.5 | 35.5;  300 40.4 | 43.8 | 44.2;  800 102 | 94 | 100;  2,048 246 | 198 | 246
 static Cut grad_cut(int64_t n, int V, bool bf16) {
-    const Cut c = rows_cut(n, V, bf16);
+    const Cut c = rows_cut(n, V, bf16, false);
     if (c == HELD || c == PARTS || V < HELD_LEAST) return c;
-    const bool fits = V <= (bf16 ? 131072 : 65536), is_long = (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024;
-    if (fits && (n <= CUS || (is_long && n >= 3 * CUS / 2))) return HELD;
-    return n < 3 * CUS / 2 ? PARTS : WHOLE;
+    const bool fits = V <= (bf16 ? 131072 : 65536);
+    if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= MEET_ROWS))) return HELD;
+    return n < MEET_ROWS ? PARTS : WHOLE;
+}
+// The loss alone: as log-probabilities, but little more than one row to a compute unit in parts that a second launch joins (300 rows of 50,001 fp32 entries 16.7 us;
+// in one launch, whose parts wait for what they leave to arrive, 19.9, wide 20.5, whole 20.9), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
+static Cut loss_cut(int64_t n, int V, bool bf16) {
+    const Cut c = rows_cut(n, V, bf16, true);
+    return c == AHEAD || (c == WIDE && n > CUS) ? n < MEET_ROWS ? PARTS : c == WIDE ? WIDE : WHOLE : c;
 }
 template <bool BF16, bool GRAD>
 static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
@@ -687,7 +717,7 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
         constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
         launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
     };
-    const Cut cut = GRAD ? grad_cut(a.n, a.V, BF16) : rows_cut(a.n, a.V, BF16);
+    const Cut cut = GRAD ? grad_cut(a.n, a.V, BF16) : loss_cut(a.n, a.V, BF16);
     if (cut == HELD && a.V <= HELD_V) {
         by_held(a.V, held);
     } else if (cut == HELD) {
@@ -696,12 +726,19 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
             else if constexpr (BF16) held(Held<1024, 16>());
         }
     } else if (cut == PARTS) {
-        launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, !GRAD>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
+        const dim3 grid((u32)(a.n * a.parts));
+        if (!GRAD && a.n < PARTS_ROWS) {
+            launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
+            return hipGetLastError();
+        }
+        launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || !GRAD) return e;
-        launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
+        if (e != hipSuccess) return e;
+        if constexpr (GRAD) launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, grid, dim3(STREAM_NT), 0, a);
+        else launch_kernel(KID_DISTILL_JOIN, st, distill_loss_kernel, dim3((u32)a.n), dim3(64), 0, a);
     } else if (cut == WIDE) {
-        if constexpr (!GRAD) launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, false, WIDE_NT>, dim3((u32)a.n), dim3(WIDE_NT), 0, a);
+        if constexpr (!GRAD)
+            launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, false, WIDE_NT>, dim3((u32)a.n), dim3(WIDE_NT), 0, a);
     } else {
         launch_kernel(KID_DISTILL, st, distill_stream_kernel<BF16, GRAD, STREAM_NT>, dim3((u32)a.n), dim3(STREAM_NT), 0, a);
     }
@@ -711,7 +748,7 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
 // Sums of the parts, then their marks or, with the gradient, the elements of S: as many as parts can be, as for logprob_workspace.
 size_t distill_workspace(int64_t n, int V) {
     const size_t goes = row_goes(V);
-    return (size_t)std::min(n, 3 * CUS / 2 - 1) * (goes * 8 + std::max<size_t>(goes * 8, DT_DISTILL_K_MAX * sizeof(float)));
+    return (size_t)std::min(n, MEET_ROWS - 1) * (goes * 8 + std::max<size_t>(goes * 8, DT_DISTILL_K_MAX * sizeof(float)));
 }
 hipError_t distill_launch(DistillArgs a, hipStream_t st) {
     a.part_goes = part_goes(a.n, a.V);

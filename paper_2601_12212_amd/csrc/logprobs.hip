@@ -304,9 +304,9 @@ __device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row
 
 extern __shared__ __align__(16) unsigned char lp_lds[];
 
-// Whole rows.
-template <bool BF16, bool ENT, bool TOP, int NT>
-__global__ __launch_bounds__(NT, 8) void logprob_stream_kernel(LogprobArgs a) {
+// Whole rows.  ASK: a go is asked for while the one before is worked on.
+template <bool BF16, bool ENT, bool TOP, int NT, bool ASK>
+__global__ __launch_bounds__(NT, ASK ? 4 : 8) void logprob_stream_kernel(LogprobArgs a) {
     constexpr int U = STREAM_U;
     const int64_t e = blockIdx.x;
     const int tid = threadIdx.x;
@@ -331,11 +331,14 @@ __global__ __launch_bounds__(NT, 8) void logprob_stream_kernel(LogprobArgs a) {
     float mine = -INFINITY;
     const int goes = row.template goes<NT * U>();
     bool zeros = false;
+    Raw<BF16, U> raw, next;
+    if (ASK && goes > 0) go_request<NT, false>(row, 0, raw);
     for (int it = 0; it < goes; ++it) {
-        Raw<BF16, U> raw;
-        go_request<NT, false>(row, it, raw);
+        if (ASK) go_request<NT, false>(row, min(it + 1, goes - 1), next);
+        else go_request<NT, false>(row, it, raw);
         float x[8 * U];
         go_take<NT, U>(row, it, raw, 0, x);
+        if (ASK) raw = next;
         const float mx = max_of(x);
         if (TOP) {
             slots[it * NT] = (uint16_t)(ord32(mx) >> 16);
@@ -450,12 +453,13 @@ __global__ __launch_bounds__(STREAM_NT, 8) void logprob_parts_kernel(LogprobArgs
 
 template <bool BF16, bool ENT, bool TOP>
 static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
-    const auto whole = [&](auto nt) {
+    const auto whole = [&](auto nt, auto ask) {
         constexpr int NT = decltype(nt)::value;
+        constexpr bool ASK = decltype(ask)::value;
         const size_t goes = (a.V + NT * STREAM_U * 8 - 1) / (NT * STREAM_U * 8), lds = TOP ? sizeof(TopRoom<NT>) + goes * NT * 2 : 0;
-        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, NT>, dim3((u32)a.n), dim3(NT), lds, a);
+        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, NT, ASK>, dim3((u32)a.n), dim3(NT), lds, a);
     };
-    switch (rows_cut(a.n, a.V, BF16)) {
+    switch (rows_cut(a.n, a.V, BF16, a.row_of != nullptr)) {
         case HELD:
             by_held(a.V, [&](auto h) {
                 constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
@@ -465,8 +469,9 @@ static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
         case PARTS:
             launch_kernel(KID_LOGPROBS, st, logprob_parts_kernel<BF16, ENT, TOP>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
             break;
-        case WIDE: whole(std::integral_constant<int, WIDE_NT>()); break;
-        case WHOLE: whole(std::integral_constant<int, STREAM_NT>()); break;
+        case WIDE: whole(std::integral_constant<int, WIDE_NT>(), std::false_type()); break;
+        case AHEAD: whole(std::integral_constant<int, STREAM_NT>(), std::true_type()); break;
+        case WHOLE: whole(std::integral_constant<int, STREAM_NT>(), std::false_type()); break;
     }
     return hipGetLastError();
 }

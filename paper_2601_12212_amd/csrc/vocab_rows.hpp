@@ -288,19 +288,25 @@ enum Cut {
     HELD,   // a workgroup holds a row: one launch, read once, whatever the number of rows
     PARTS,  // a row is many workgroups', which meet
     WIDE,   // whole rows, 1,024 threads to each
+    AHEAD,  // whole rows, 256 threads to each, a go asked for while the one before is worked on
     WHOLE   // whole rows, 256 threads to each
 };
-// Rows that are streamed: few are cut, so that they fill the chip; while there is one to a compute unit, or up to eight of 160 KB and more, its
-// reading is what takes the time, and 1,024 threads read it; else rows are there by the thousand, and eight small workgroups to a compute unit overlap one's
-// end with another's reading.  Log-probabilities of n rows of V bf16 entries, us, with no / 20 alternatives, in parts | wide | whole:
-//     V = 50,001:  n = 64 7.3 / 11.6 | 9.1 / 12.4 | 10.8 / 15.1;  200 9.5 / 15.8 | 9.8 / 13.1 | 11.6 / 15.5;  500 14.4 / 22.5 | 15.9 / 19.1 | 13.9 / 18.1
-//     V = 128,256: n = 64 8.8 / 14.1 | 12.1 / 15.8 | 20.4 / 25.2;  200 15.0 / 22.8 | 13.3 / 16.6 | 21.7 / 26.4;  1,200 55.7 / 74.2 | 53.0 / 60.1 | 54.1 / 59.9
+// Rows that are streamed: few are cut, so that they fill the chip; with one row to a compute unit 1,024 threads read it; with two, 256 threads that ask ahead;
+// beyond that rows are there by the thousand, and eight small workgroups to a compute unit overlap one's end with another's reading, with as few registers as that takes.
+// Log-probabilities of n rows of V bf16 entries, us, with no / 20 alternatives, parts | wide | ahead | whole:
+//     V = 50,001:  n = 64 7.3 / 11.6 | 9.1 / 12.4 | - | 10.8 / 15.1;  200 9.5 / 15.8 | 9.8 / 13.1 | 8.9 / 12.6 | 11.6 / 15.5;  500 14.4 / 22.5 | 13.7 / 17.9 | 12.7 / 16.7 | 13.9 / 18.1
+//     V = 128,256: n = 64 8.8 / 14.1 | 12.1 / 15.8 | - | 20.4 / 25.2;  200 15.0 / 22.8 | 13.3 / 16.6 | 15.0 / 19.1 | 21.7 / 26.4;  500 27 / 38 | 25.9 / 28.8 | 23.8 / 27.6 | 26.3 / 31.1;
+//                  2,048 83 / 106 | 83.7 / 93.5 | 89.7 / 96.9 | 83.2 / 90.5
+// some_none: rows that are named one by one, of which some are none.  Then the next workgroup has to take a place that is free: long rows, the emitted ones of 64
+// sequences, 281 of 576, were 24.4 us wide, where two fit a compute unit, and 30.5 by 256 threads, where those that come to a compute unit at first stay.
 constexpr int64_t PARTS_ROWS = 128, CUS = 256, MANY_ROWS = 2048;
-inline Cut rows_cut(int64_t n, int V, bool bf16) {
+inline bool row_is_long(int V, bool bf16) { return (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024; }
+inline Cut rows_cut(int64_t n, int V, bool bf16, bool some_none) {
     if (V >= HELD_LEAST && V <= HELD_V) return HELD;
     if (V < HELD_LEAST) return WHOLE;
     if (n < PARTS_ROWS) return PARTS;
-    return n <= CUS || (n < MANY_ROWS && (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024) ? WIDE : WHOLE;
+    if (n <= CUS || (some_none && n < MANY_ROWS && row_is_long(V, bf16))) return WIDE;
+    return n <= 2 * CUS ? AHEAD : WHOLE;
 }
 // goes of a part, so that there are about eight workgroups to a compute unit; parts of a row (up to 64)
 inline int part_goes(int64_t n, int V) {
