@@ -249,19 +249,15 @@ typedef u32 Vec16Any2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef u32 Vec16Any4 __attribute__((ext_vector_type(4), aligned(4)));
 template <bool BF16>
 __device__ __forceinline__ void put_unit(void *grad, int64_t at, const float *g) {
+    Vec16 v;
     if constexpr (BF16) {
-        Vec16 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = to_bf16(g[2 * e], g[2 * e + 1]);
         __builtin_nontemporal_store(v, (Vec16Any2 *)((uint16_t *)grad + at));
     } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Vec16 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(g[4 * h + e]);
-            __builtin_nontemporal_store(v, (Vec16Any4 *)((float *)grad + at + 4 * h));
-        }
+        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(g[e]);
+        __builtin_nontemporal_store(v, (Vec16Any4 *)((float *)grad + at));
     }
 }
 // q (a + b log2 q) of an element, q = 2^((x - m) c - log2 s)
@@ -330,17 +326,18 @@ __device__ __forceinline__ float hide_loose(const DistillArgs &a, const Entries 
 // The gradients of a go, G units at once; at: where the row's gradient starts.
 template <int NT, int G, bool ENT, bool BF16, int U>
 __device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope &k, void *grad, int64_t at, const Raw<BF16, U> &raw) {
+    constexpr int E = Row<BF16>::E;
 #pragma unroll
     for (int first = 0; first < U; first += G) {
         float x[8 * G];
         go_take<NT, G>(row, it, raw, first, x);
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-            const int unit = (it * U + first + i) * NT + (int)threadIdx.x;
-            float g[8];
+        for (int i = 0; i < 8 * G / E; ++i) {
+            const int unit = (it * raw.N + 8 * first / E + i) * NT + (int)threadIdx.x;
+            float g[E];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = slope_at<ENT>(k, x[8 * i + e]);
-            if (unit < row.units) put_unit<BF16>(grad, at + row.head + 8 * (int64_t)unit, g);
+            for (int e = 0; e < E; ++e) g[e] = slope_at<ENT>(k, x[E * i + e]);
+            if (unit < row.units) put_unit<BF16>(grad, at + row.head + E * (int64_t)unit, g);
         }
     }
 }
@@ -461,7 +458,8 @@ __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> 
     constexpr int U = STREAM_U;
     for (int it = first; it < end; ++it) {
         if (it > first) go_request<NT, false>(row, it, raw);
-        distill_put_go<NT, U>(a, row, it, E, t, d, raw, xs);
+        go_keep(raw);
+        distill_put_go<NT, 1>(a, row, it, E, t, d, raw, xs);
     }
     if (loose) {
         const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
@@ -485,7 +483,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(
     const bool lead = threadIdx.x < 64;
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
-    const int goes = row.template goes<NT * U>();
+    const int goes = row.template goes<NT, U>();
     Given G;
     Entries E;
     entries_load(a, tr, G);
@@ -544,7 +542,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
         for (int s = 0; s < SLOTS; ++s)
             if (64 * s + lane_id() < a.k) a.s_elems[r * a.k + 64 * s + lane_id()] = xs[s];
     }
-    Sums s = sums_outside<BF16, !LAST, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<STREAM_GO>()), part == 0);
+    Sums s = sums_outside<BF16, !LAST, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
     s = block_sums<false, NT>(s, a.c, room);
     if (threadIdx.x >= 64) return;
     u64 *const sums = (u64 *)a.ws + r * a.parts;
@@ -592,7 +590,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
-    const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
+    const int end = min(first + a.part_goes, row.template goes<NT, U>());
     if (tr < 0) {
         if (part == 0) row_loss_none(a, r);
         const int from = min(part * a.part_goes * STREAM_ELEMS, a.V), to = min((part + 1) * a.part_goes * STREAM_ELEMS, a.V);
@@ -638,7 +636,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     }
     const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     const float m = a.stats[2 * r], l = a.stats[2 * r + 1], tail = a.tail[r];
-    const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
+    const int end = min(first + a.part_goes, row.template goes<NT, U>());
     Given G;
     Entries E;
     entries_load(a, tr, G);
@@ -677,11 +675,12 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
         here = place_of<BF16, NT, U>(row, y);
         if ((int)threadIdx.x == here.thread) xy = row.at(y);  // (before this thread stores anything)
     }
-    const int end = min(first + a.part_goes, row.template goes<STREAM_GO>());
+    const int end = min(first + a.part_goes, row.template goes<NT, U>());
     for (int it = first; it < end; ++it) {
         Raw<BF16, U> raw;
         go_request<NT, false>(row, it, raw);
-        put_go<NT, U, ENT>(row, it, k, a.grad, at, raw);
+        go_keep(raw);
+        put_go<NT, 1, ENT>(row, it, k, a.grad, at, raw);
         if (it == here.go && (int)threadIdx.x == here.thread) put_elem<BF16>(a.grad, at + y, slope_at<ENT>(k, xy) + g);
     }
     if (part == 0 && (int)threadIdx.x < row.loose) {

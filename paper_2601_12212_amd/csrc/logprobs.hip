@@ -237,7 +237,7 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
             if (most >= edge && most > -INFINITY)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], row.head + 8 * (u * NT + tid) + j);
+                    if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], id_of<NT, U>(row, 0, tid, 8 * u + j));
         }
     }
     __syncthreads();
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
 // Ends with a barrier; the number found.
 template <int NT, bool BF16, class Each>
 __device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row, int k, u32 mine, Each each) {
-    constexpr int U = STREAM_U;
+    constexpr int E = Row<BF16>::E, N = STREAM_U * 8 / E;
     typedef TopRoom<NT> R;
     const int tid = threadIdx.x;
     const u32 kth = top_bound<NT>(r, 0.f, k);
@@ -275,25 +275,14 @@ __device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row
     __syncthreads();
     const int hits = (int)r.hits;
     if (hits <= R::HITS)
-        for (int i = tid; i < hits * U; i += NT) {  // a unit to a thread
-            const int s = (int)r.hit[i / U], unit = ((s / NT) * U + i % U) * NT + s % NT;
+        for (int i = tid; i < hits * N; i += NT) {  // a unit to a thread
+            const int s = (int)r.hit[i / N], unit = ((s / NT) * N + i % N) * NT + s % NT;
             if (unit >= row.units) continue;
-            const int at = row.head + 8 * unit;
-            float x[8];
-            const Vec16 *q = (const Vec16 *)(row.p + at);
-            const Vec16 lo = q[0], hi = BF16 ? lo : q[1];
+            const int at = row.head + E * unit;
+            float x[E];
+            unpack(*(const Vec16 *)(row.p + at), x);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (BF16) {
-                    x[2 * j] = __uint_as_float(lo[j] << 16);
-                    x[2 * j + 1] = __uint_as_float(lo[j] & 0xFFFF0000u);
-                } else {
-                    x[j] = __uint_as_float(lo[j]);
-                    x[4 + j] = __uint_as_float(hi[j]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < E; ++j)
                 if (x[j] >= edge && x[j] > -INFINITY) top_keep(r, x[j], at + j);
         }
     __syncthreads();
@@ -329,7 +318,7 @@ __global__ __launch_bounds__(NT, ASK ? 4 : 8) void logprob_stream_kernel(Logprob
     }
     Sums r = {-INFINITY, 0.f, 0.f};
     float mine = -INFINITY;
-    const int goes = row.template goes<NT * U>();
+    const int goes = row.template goes<NT, U>();
     bool zeros = false;
     Raw<BF16, U> raw, next;
     if (ASK && goes > 0) go_request<NT, false>(row, 0, raw);
@@ -377,7 +366,7 @@ __global__ __launch_bounds__(STREAM_NT, 8) void logprob_parts_kernel(LogprobArgs
     const Row<BF16> row(a.logits, at, a.V);
     u64 *const slots = a.slots + e * a.goes * WORDS;
     Sums r = {-INFINITY, 0.f, 0.f};
-    const int goes = row.template goes<STREAM_GO>(), end = min((part + 1) * a.part_goes, goes);
+    const int goes = row.template goes<NT, U>(), end = min((part + 1) * a.part_goes, goes);
     bool zeros = false;
     for (int it = part * a.part_goes; it < end; ++it) {
         Raw<BF16, U> raw;

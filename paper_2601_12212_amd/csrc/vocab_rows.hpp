@@ -1,8 +1,8 @@
 // A workgroup's pass over a row of logits: what the log-probabilities (logprobs.hip) and the losses and gradients (distill.hip) share.
 //
-// A row is V elements from any address.  Elements up to the first multiple of 16 bytes and behind the last whole unit of eight are `loose`, up to 14, one
-// to a thread; the units are read 16 bytes at a time.  A thread takes U units at a go, NT units apart, so that a go of a workgroup of NT threads reads
-// NT * U * 8 elements front to back.
+// A row is V elements from any address.  Elements up to the first multiple of 16 bytes and behind the last whole unit of 16 bytes are `loose`, up to 14, one
+// to a thread.  A thread takes 8 U elements at a go, in units NT apart, so that a go of a workgroup of NT threads reads NT * U * 8 elements front to back, and every
+// load of a wave 1 KB side by side.  (Units of eight fp32 elements, 32 bytes to a lane: gradients of 2,048 rows of 32,000 108 us.)
 //
 // Softmax statistics.  With c = log2(e) / T a row's weights are 2^(x c - M2), M2 = fl(m c) for the largest logit m so far: one fused multiply-add
 // and one exp2 an element, and since every sum refers to the M2 that was subtracted, its rounding drops out of all results.  Sums are fp32.
@@ -33,21 +33,21 @@ struct Elem<false> {
 
 template <bool BF16>
 struct Row {
+    static constexpr int E = BF16 ? 8 : 4;  // elements of a unit
     const typename Elem<BF16>::T *p;
     int V, head, units, loose;
     __device__ __forceinline__ Row(const void *logits, int64_t at, int n) {
         p = (const typename Elem<BF16>::T *)logits + at;
         V = n;
-        const int per16 = BF16 ? 8 : 4;
-        head = min((int)(-(uintptr_t)p / sizeof(*p)) & (per16 - 1), n);
-        units = (n - head) >> 3;
-        loose = n - 8 * units;
+        head = min((int)(-(uintptr_t)p / sizeof(*p)) & (E - 1), n);
+        units = (n - head) / E;
+        loose = n - E * units;
     }
     __device__ __forceinline__ float at(int i) const { return Elem<BF16>::get(p + i); }
     // where loose element i, i < loose, lies in the row
-    __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + 8 * units; }
-    template <int GO>
-    __device__ __forceinline__ int goes() const { return (units + GO - 1) / GO; }
+    __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + E * units; }
+    template <int NT, int U>
+    __device__ __forceinline__ int goes() const { return (E * units + NT * U * 8 - 1) / (NT * U * 8); }
 };
 
 // Where element `id` is worked on: at go `go` (-1: a loose one) by thread `thread`, as its element `elem`.
@@ -56,61 +56,76 @@ struct Place {
 };
 template <bool BF16, int NT, int U>
 __device__ __forceinline__ Place place_of(const Row<BF16> &row, int id) {
+    constexpr u32 E = Row<BF16>::E, GO = NT * U * 8 / E;  // units of a go
     const u32 at = (u32)(id - row.head);
-    if (at >= 8u * (u32)row.units) return Place{-1, id < row.head ? id : id - 8 * row.units, 0};
-    const u32 unit = at >> 3, in_go = unit % (NT * U);
-    return Place{(int)(unit / (NT * U)), (int)(in_go % NT), (int)(8 * (in_go / NT) + (at & 7))};
+    if (at >= E * (u32)row.units) return Place{-1, id < row.head ? id : id - (int)E * row.units, 0};
+    const u32 unit = at / E, in_go = unit % GO;
+    return Place{(int)(unit / GO), (int)(in_go % NT), (int)(E * (in_go / NT) + at % E)};
+}
+// the id of a thread's element `elem` of go `it`
+template <int NT, int U, bool BF16>
+__device__ __forceinline__ int id_of(const Row<BF16> &row, int it, int thread, int elem) {
+    constexpr int E = Row<BF16>::E;
+    return row.head + E * ((it * (U * 8 / E) + elem / E) * NT + thread) + elem % E;
 }
 
 typedef u32 Vec16 __attribute__((ext_vector_type(4)));
 template <bool BF16, int U>
 struct Raw {
-    Vec16 r[U][BF16 ? 1 : 2];
+    static constexpr int N = U * 8 / Row<BF16>::E;
+    Vec16 r[N];
 };
 // the units of go `it` of this thread; those past the end are the last unit again (row.units > 0)
 template <int NT, bool KEEP, bool BF16, int U>
 __device__ __forceinline__ void go_request(const Row<BF16> &row, int it, Raw<BF16, U> &raw) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int unit = min((it * U + u) * NT + (int)threadIdx.x, row.units - 1);
-        const Vec16 *q = (const Vec16 *)(row.p + row.head + 8 * (int64_t)unit);
-#pragma unroll
-        for (int h = 0; h < (BF16 ? 1 : 2); ++h) raw.r[u][h] = KEEP ? q[h] : __builtin_nontemporal_load(q + h);
+    for (int u = 0; u < raw.N; ++u) {
+        const int unit = min((it * raw.N + u) * NT + (int)threadIdx.x, row.units - 1);
+        const Vec16 *q = (const Vec16 *)(row.p + row.head + row.E * (int64_t)unit);
+        raw.r[u] = KEEP ? *q : __builtin_nontemporal_load(q);
     }
     __builtin_amdgcn_sched_barrier(0);  // all on their way before anything that follows
 }
-// units first .. first + G - 1 of what was read, as floats; of units past the end -inf
+__device__ __forceinline__ void unpack(const Vec16 &v, float (&x)[8]) {  // bf16
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(v[e] << 16);
+        x[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const Vec16 &v, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(v[e]);
+}
+// elements 8 first .. 8 (first + G) - 1 of what was read, as floats; of units past the end -inf
 template <int NT, int G, bool BF16, int U>
 __device__ __forceinline__ void go_take(const Row<BF16> &row, int it, const Raw<BF16, U> &raw, int first, float (&x)[8 * G]) {
+    constexpr int E = Row<BF16>::E, N = 8 * G / E;
+    const int from = 8 * first / E;
 #pragma unroll
-    for (int u = 0; u < G; ++u)
+    for (int u = 0; u < N; ++u) {
+        float y[E];
+        unpack(raw.r[from + u], y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (BF16) {
-                x[8 * u + 2 * e] = __uint_as_float(raw.r[first + u][0][e] << 16);
-                x[8 * u + 2 * e + 1] = __uint_as_float(raw.r[first + u][0][e] & 0xFFFF0000u);
-            } else {
-                x[8 * u + e] = __uint_as_float(raw.r[first + u][0][e]);
-                x[8 * u + 4 + e] = __uint_as_float(raw.r[first + u][1][e]);
-            }
-        }
-    if ((it * U + first + G) * NT > row.units) {  // uniform
+        for (int e = 0; e < E; ++e) x[E * u + e] = y[e];
+    }
+    if ((it * raw.N + from + N) * NT > row.units) {  // uniform
         asm volatile("");  // (a branch, and not a choice for every element)
 #pragma unroll
-        for (int u = 0; u < G; ++u) {
-            const bool there = (it * U + first + u) * NT + (int)threadIdx.x < row.units;
+        for (int u = 0; u < N; ++u) {
+            const bool there = (it * raw.N + from + u) * NT + (int)threadIdx.x < row.units;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[8 * u + e] = there ? x[8 * u + e] : -INFINITY;
+            for (int e = 0; e < E; ++e) x[E * u + e] = there ? x[E * u + e] : -INFINITY;
         }
     }
 }
 
-// Between two passes over what was read: else the compiler keeps the first pass's floats, twice the registers of bf16 elements.
+// Between two passes over what was read: else the compiler keeps the first pass's floats, twice the registers of bf16 elements.  And before what is read is worked
+// on and stored unit by unit: all of it has arrived then.
 template <bool BF16, int U>
 __device__ __forceinline__ void go_keep(Raw<BF16, U> &raw) {
-    if (BF16)
 #pragma unroll
-        for (int u = 0; u < U; ++u) asm("" : "+v"(raw.r[u][0]));
+    for (int u = 0; u < raw.N; ++u) asm("" : "+v"(raw.r[u]));
 }
 
 // Sums of a part of a row against its largest logit m: s = sum 2^(x c - M2), w = sum 2^(x c - M2) (x c - M2).
@@ -269,7 +284,7 @@ __device__ __forceinline__ void parts_leave(u64 *marks, int parts) {
 
 // ---- how a call of n rows is cut -------------------------------------------------------------------
 // A go of a workgroup that streams reads 8,192 elements, 16 or 32 KB; with four times the threads, four times that.
-constexpr int STREAM_NT = 256, WIDE_NT = 1024, STREAM_U = 4, STREAM_GO = STREAM_NT * STREAM_U, STREAM_ELEMS = 8 * STREAM_GO;
+constexpr int STREAM_NT = 256, WIDE_NT = 1024, STREAM_U = 4, STREAM_ELEMS = 8 * STREAM_NT * STREAM_U;
 inline int row_goes(int V) { return (V + STREAM_ELEMS - 1) / STREAM_ELEMS; }
 // Workgroups that hold a row in their registers: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries.
 template <int NT_, int U_>
