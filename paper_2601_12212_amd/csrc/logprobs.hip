@@ -22,17 +22,40 @@ struct TopRoom {
     u32 n, hits, kth, need, prefix;
     u32 tm[256];           // the threads' largest, 16-bit keys, two threads' as one where there are more
     u32 counts[NT / 64];
-    u32 hit[HITS];         // slots that reach the bound
     union {
-        u64 keys[CAP];     // candidates
+        u32 hit[HITS];     // slots that reach the bound
         u32 hist[256];
     };
+    u64 keys[CAP];         // candidates
+};
+// Eights of a held row with an element that reaches the bound, and whose they are.
+template <int NT>
+struct TopEights {
+    static constexpr int CAP = NT == 64 ? 64 : 128;
+    float x[CAP][8];
+    u32 whose[CAP];        // thread and unit
 };
 
 template <int NT>
 __device__ __forceinline__ void top_keep(TopRoom<NT> &r, float x, int id) {
     const u32 at = atomicAdd(&r.n, 1u);
     if (at < TopRoom<NT>::CAP) r.keys[at] = make_key(x, (u32)id);
+}
+
+// those of x that reach `edge`, by one step of the list's end
+template <int NT, int N, class Id>
+__device__ __forceinline__ void top_keep_of(TopRoom<NT> &r, const float (&x)[N], float edge, Id id) {
+    u32 some = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) some |= (u32)(x[j] >= edge && x[j] > -INFINITY) << j;
+    if (!some) return;
+    u32 at = atomicAdd(&r.n, (u32)__popc(some));
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (some >> j & 1u) {
+            if (at < TopRoom<NT>::CAP) r.keys[at] = make_key(x[j], (u32)id(j));
+            ++at;
+        }
 }
 
 // Radix selection: exactly the k best of a row that holds more than k finite entries.
@@ -130,7 +153,9 @@ __device__ __forceinline__ void ranked(const u64 *keys, int n, int k, F f) {
         const int lane = lane_id();
         const u64 key = lane < n ? keys[lane] : 0ull;
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += readlane_u64(key, j) > key;
+        for (int j0 = 0; j0 < n; j0 += 8)  // lanes past the n-th hold 0, which is above none
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rank += readlane_u64(key, j0 + j) > key;
         if (lane < n && rank < k) f(rank, key);
         if (lane >= n && lane < k) f(lane, 0ull);
         return;
@@ -183,13 +208,15 @@ __device__ __forceinline__ void alternatives_write(const LogprobArgs &a, int64_t
 }
 
 // ---- rows that a workgroup holds ----
+// Waves of a SIMD: as many as leave a thread its registers, but a few spilled ones with TOP (8,000 bf16 rows of 21,840, k 1: 97 us at 6, 122 at 5).
 template <bool BF16, bool ENT, bool TOP, int NT, int U>
-__global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob_held_kernel(LogprobArgs a) {
-    constexpr int G = U == 4 ? 4 : 2;  // units that are worked on at once
+__global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : ENT && U == 8 ? 7 : 8) void logprob_held_kernel(LogprobArgs a) {
+    constexpr int G = 2;  // units that are worked on at once: with four, registers go to scratch, and 8,000 fp32 rows of 6,000 (k 20) take 98 us for 48
     const int64_t e = blockIdx.x;
     const int tid = threadIdx.x;
     __shared__ Sums s_sums[NT / 64];
     __shared__ TopRoom<TOP ? NT : 64> room_;
+    __shared__ TopEights<NT> eights;
     TopRoom<NT> &room = (TopRoom<NT> &)room_;
     const int64_t at = entry_row(a, e);
     if (at < 0) {
@@ -202,7 +229,7 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
     const float xl = tid < row.loose ? row.at(row.loose_at(tid)) : -INFINITY;
     const float xy = token_logit<BF16>(a, e, at);
     if (TOP) {
-        if (tid == 0) room.n = 0;
+        if (tid == 0) room.n = room.hits = 0;
         if (NT > 256) {
             if (tid < 256) room.tm[tid] = NO_KEY;
             __syncthreads();
@@ -227,22 +254,43 @@ __global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : 8) void logprob
     if (tid == NT - 1) entry_write(a, e, xy, r, st);
     if (!TOP) return;
     const float edge = key_edge(top_bound<NT>(room, mine, a.k));
+    // The few eights that reach the bound go through LDS: a branch for each of a thread's elements is long code that is met for the first time
+    // (one bf16 row of 21,840, k 31: 10.5 us, and 8.9 so).
     if (mine >= edge && mine > -INFINITY) {
         if (xl >= edge && xl > -INFINITY) top_keep(room, xl, row.loose_at(tid));
+        u32 some = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float x[8];
             go_take<NT, 1>(row, 0, raw, u, x);
             const float most = max_of(x);
-            if (most >= edge && most > -INFINITY)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (x[j] >= edge && x[j] > -INFINITY) top_keep(room, x[j], id_of<NT, U>(row, 0, tid, 8 * u + j));
+            some |= (u32)(most >= edge && most > -INFINITY) << u;
         }
+        u32 put = atomicAdd(&room.hits, (u32)__popc(some));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (some >> u & 1u) {
+                if (put < TopEights<NT>::CAP) {
+                    float x[8];
+                    go_take<NT, 1>(row, 0, raw, u, x);
+                    eights.whose[put] = (u32)(tid * U + u);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) eights.x[put][j] = x[j];
+                }
+                ++put;
+            }
     }
     __syncthreads();
+    const int hits = (int)room.hits;
+    if (hits <= TopEights<NT>::CAP)
+        for (int i = tid; i < 8 * hits; i += NT) {
+            const float x = eights.x[i >> 3][i & 7];
+            const u32 whose = eights.whose[i >> 3];
+            if (x >= edge && x > -INFINITY) top_keep(room, x, id_of<NT, U>(row, 0, (int)(whose / U), 8 * (int)(whose % U) + (i & 7)));
+        }
+    __syncthreads();
     int found = (int)room.n;
-    if (found > TopRoom<NT>::CAP) {
+    if (hits > TopEights<NT>::CAP || found > TopRoom<NT>::CAP) {
         top_by_radix<BF16, NT>(room, row.p, a.V, a.k);
         found = (int)room.n;
     }
@@ -281,9 +329,7 @@ __device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row
             const int at = row.head + E * unit;
             float x[E];
             unpack(*(const Vec16 *)(row.p + at), x);
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (x[j] >= edge && x[j] > -INFINITY) top_keep(r, x[j], at + j);
+            top_keep_of(r, x, edge, [&](int j) { return at + j; });
         }
     __syncthreads();
     if (hits <= R::HITS && (int)r.n <= R::CAP) return (int)r.n;
