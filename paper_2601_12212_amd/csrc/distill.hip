@@ -701,7 +701,7 @@ static Cut grad_cut(int64_t n, int V, bool bf16) {
     const Cut c = rows_cut(n, V, bf16, false);
     if (c == HELD || c == PARTS || V < HELD_LEAST) return c;
     const bool fits = V <= (bf16 ? 131072 : 65536);
-    if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= MEET_ROWS))) return HELD;
+    if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= MEET_ROWS && launch_holds(n, 1024)))) return HELD;
     return n < MEET_ROWS ? PARTS : WHOLE;
 }
 // The loss alone: as log-probabilities, but little more than one row to a compute unit in parts that a second launch joins (300 rows of 50,001 fp32 entries 16.7 us;

@@ -299,6 +299,8 @@ inline void by_held(int V, F f) {
     else f(Held<512, 8>());
 }
 constexpr int HELD_LEAST = 32, HELD_V = 32768;  // (shorter rows may have no whole unit)
+// A launch has fewer than 2^32 threads.  (Rows are fewer than 2^24: only workgroups of more than 256 come there.)
+inline bool launch_holds(int64_t n, int nt) { return n * nt < (int64_t)1 << 32; }
 enum Cut {
     HELD,   // a workgroup holds a row: one launch, read once, whatever the number of rows
     PARTS,  // a row is many workgroups', which meet
@@ -317,7 +319,7 @@ enum Cut {
 constexpr int64_t PARTS_ROWS = 128, CUS = 256, MANY_ROWS = 2048;
 inline bool row_is_long(int V, bool bf16) { return (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024; }
 inline Cut rows_cut(int64_t n, int V, bool bf16, bool some_none) {
-    if (V >= HELD_LEAST && V <= HELD_V) return HELD;
+    if (V >= HELD_LEAST && V <= HELD_V && (V <= 16384 || launch_holds(n, 512))) return HELD;
     if (V < HELD_LEAST) return WHOLE;
     if (n < PARTS_ROWS) return PARTS;
     if (n <= CUS || (some_none && n < MANY_ROWS && row_is_long(V, bf16))) return WIDE;

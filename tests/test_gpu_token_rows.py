@@ -471,3 +471,102 @@ def test_a_step_says_what_it_emitted_and_what_the_draft_can_learn():
             d = 3 * ref.delta(st.V)                        # the teacher's values have been rounded and summed once more
             ref.close(loss[r0:r1], want["loss"], d * want["terms"], "loss")
             ref.close(grad[r0:r1], want["grad"], ref.HALF[st.dtype] * want["grad"].abs() + 8 * d * want["size"] + ref.TINY, "grad")
+
+
+# How rows are cut among workgroups goes by their number, length and type: one of each kind, and the edges between them.
+CUTS = [(127, 33001, 3), (128, 33001, 3), (200, 50003, 0), (256, 40001, 20), (257, 40001, 1), (300, 33001, 20), (512, 32769, 0), (513, 33003, 4),
+        (600, 50001, 20), (3000, 31, 3), (100, 16384, 7), (100, 16385, 7), (90, 32768, 31)]
+
+
+@pytest.mark.parametrize("n, V, k", CUTS)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_logprobs_by_number_of_rows(n, V, k, dtype):
+    x, xd = rows(n, V, dtype, n + V, offset=1, pad=2)
+    tokens = torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(V), dtype=torch.int32)
+    got = run_logprobs(xd[None], None, tokens.to(DEV)[None], 1.0, k, n)
+    some = torch.unique(torch.cat([torch.arange(0, n, max(1, n // 40)), torch.tensor([n - 1])]))
+    check_logprobs({name: v[:, some.to(DEV)] for name, v in got.items()}, x[some], tokens[some], 1.0, k)
+
+
+@pytest.mark.parametrize("V", [41001, 90001])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B, per", [(5, 8), (7, 40), (9, 80)])
+def test_chosen_rows_by_their_number(B, per, V, dtype):
+    """Long rows that are named one by one, half of them none: entries in parts, wide, whole."""
+    R, k = 4, 5
+    x, xd = rows(B * R, V, dtype, V + B)
+    g = torch.Generator().manual_seed(per)
+    of = torch.randint(-R, R, (B, per), generator=g, dtype=torch.int32)
+    tok = torch.randint(0, V, (B, per), generator=g, dtype=torch.int32)
+    got = run_logprobs(xd.view(B, R, V), of.to(DEV), tok.to(DEV), 0.8, k, per)
+    none = (of < 0).to(DEV)
+    assert (got["logprob"][none] == 0).all() and (got["stats"][none] == 0).all() and (got["top_id"][none] == -1).all()
+    for b in (0, B - 1):
+        keep = of[b] >= 0
+        at = keep.nonzero()[:, 0].to(DEV)
+        check_logprobs({name: v[b:b + 1, at] for name, v in got.items()}, x[b * R + of[b][keep].long()], tok[b][keep], 0.8, k)
+
+
+def test_more_entries_than_a_launch_of_large_workgroups_has():
+    """2^23 entries of 16,385: by 512 threads each they would be 2^32."""
+    n, V = 1 << 23, 16385
+    x, xd = rows(2, V, BF16, 1)
+    of = torch.arange(n, dtype=torch.int32, device=DEV) % 3 - 1
+    stats = dirty(1, n, 2)
+    dt.dt_token_logprobs(xd[None], of[None], None, 1.0, 0, None, None, stats, None, None, workspace(n, V))
+    torch.cuda.synchronize()
+    got = stats[0]
+    ref.close(got[1:3, 1], ref.logprobs(x, torch.zeros(2, **i32), 1.0, 1)["stats"][:, 1], ref.delta(V))
+    assert (got[0::3] == 0).all() and (got[1::3] == got[1]).all() and (got[2::3] == got[2]).all()
+
+
+DISTILL_CUTS = [(127, 33001), (130, 33001), (130, 65536), (130, 70001), (256, 40001), (257, 40001), (300, 33001), (383, 32769), (384, 33003), (400, 41001),
+                (400, 82001), (90, 32768), (90, 16385)]
+
+
+@pytest.mark.parametrize("n, V", DISTILL_CUTS)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_distill_by_number_of_rows(n, V, dtype):
+    k, T = 9, 1.3
+    x, xd = rows(n, V, dtype, n + V, offset=3, pad=1)
+    val, ids, lse = teacher(n, V, k, V + n)
+    w = torch.rand(n, generator=torch.Generator().manual_seed(n))
+    some = torch.unique(torch.cat([torch.arange(0, n, max(1, n // 12)), torch.tensor([1, 2, n - 1])]))
+    want = ref.distill(x[some], val[some], ids[some], lse[some], None, T, 1, w[some])
+    pick = lambda o: {name: v[some.to(DEV)] for name, v in o.items()}
+    check_distill(pick(run_distill(xd, val, ids, lse, None, T, 1, w, True)), want, dtype, V)
+    check_distill(pick(run_distill(xd, val, ids, lse, None, T, 1, None, False)), want, dtype, V)
+    same = put(x, 3, 1)                                   # in the logits' own place
+    check_distill(pick(run_distill(same, val, ids, lse, None, T, 1, w, True, grad=same)), want, dtype, V)
+
+
+@pytest.mark.parametrize("n, m, V", [(20, 3, 50003), (100, 127, 33001), (300, 40, 33001), (200, 300, 40001), (5, 6, 300001)])
+def test_graphs_that_share_a_workspace(n, m, V):
+    """Two captured calls with one workspace, replayed in turn on one stream with a third call of other sizes between them."""
+    one, run_one = _chain(n, V, 5, n)
+    two, run_two = _chain(m, V, 2, m + 7)
+    third, run_third = _chain(4, V // 2, 3, 1)
+    ws = workspace(max(n, m), V)
+    one["ws"] = two["ws"] = third["ws"] = ws
+    first, graphs = [], []
+    for b, run in ((one, run_one), (two, run_two)):
+        run()
+        torch.cuda.synchronize()
+        first.append({name: b[name].clone() for name in OUT})
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        graphs.append(graph)
+    want = ref.logprobs(one["ys"][:3].cpu(), torch.zeros(3, **i32), 1.0, 5)
+    assert torch.equal(first[0]["ti"][0, :3].cpu(), want["top_id"])
+    for i in (0, 1, 1, 0, 0, 1):
+        for b in (one, two):
+            for name in OUT:
+                b[name].fill_(3)
+        graphs[i].replay()
+        run_third()
+        graphs[1 - i].replay()
+        torch.cuda.synchronize()
+        for b, f in zip((one, two), first):
+            for name in OUT:
+                assert torch.equal(b[name].view(torch.uint8), f[name].view(torch.uint8)), (i, name)
