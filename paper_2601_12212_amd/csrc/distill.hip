@@ -190,31 +190,49 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
 }
 
 // ---- the loss ----
-// What the second pass over a row goes by.
+// q (a + b log2 q) of an element, q = 2^((x - m) c - log2 s)
+struct Slope {
+    float m, log2s, c, a, b;
+};
+__device__ __forceinline__ Slope slope(float m, float l, float c, float a, float b) {
+    // (nothing finite in the row: every q is 0)
+    return m == -INFINITY ? Slope{0.f, INFINITY, c, a, b} : Slope{m, l * LOG2E, c, a, b};
+}
+// What the gradients of a row with a teacher go by.  Outside S the gradient is q_j (P - p_t (1 - q_t) / q_t): q_j / q_t, which the sums outside S give, times
+// P q_t - p_t q_in with q_in = 1 - q_t, a sum of its own.  Neither factor leaves fp32's range, and where a student is near its teacher only
+// P and q_in, or p_t and q_t, meet, which are small and known to their last digits.
+struct DistillSlope {
+    Slope out, in;
+    float w;
+    int64_t at;
+};
+// From the row's sums in S and outside, by any thread.
 struct RowLoss {
     RowStat st;
-    float sum_in, sum_out;  // the row's sums in S and outside
-    float in_s, out;        // factors of q_j in S and outside, w / T in them
+    float q_in, q_out;  // of the student
+    Sums out;
 };
-// from the row's sums in S and outside, by any thread
-__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, float w, const Teacher &t, Sums out) {
-    Sums in = {t.in_m, t.in_s, 0.f};
+__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const Teacher &t, const Sums &out) {
+    Sums in = {t.in_m, t.in_s, 0.f}, o = out;
     const float m = fmaxf(in.m, out.m);
     sums_move<false>(in, m, a.c);
-    sums_move<false>(out, m, a.c);
-    const float whole = in.s + out.s;
+    sums_move<false>(o, m, a.c);
+    const float whole = in.s + o.s, part = whole > 0.f ? 1.f / whole : 0.f;
     RowLoss R;
     R.st = row_stat(m, whole, a.c);
-    R.sum_in = in.s;
-    R.sum_out = out.s;
-    R.in_s = w * (t.P + t.rest);
-    R.out = out.s > 0.f ? R.in_s - w * t.rest * (whole / out.s) : R.in_s;
+    R.q_in = in.s * part;
+    R.q_out = o.s * part;
+    R.out = out;
     return R;
+}
+__device__ __forceinline__ DistillSlope loss_slope(const DistillArgs &a, float w, const Teacher &t, const RowLoss &R, int64_t at) {
+    const RowStat o = row_stat(R.out.m, R.out.s, a.c);
+    return DistillSlope{slope(o.m, o.l, a.c, w * (t.P * R.q_out - t.rest * R.q_in), 0.f), slope(R.st.m, R.st.l, a.c, w * (t.P + t.rest), 0.f), w, at};
 }
 // by the first wave
 __device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, const Teacher &t, const RowLoss &R) {
-    const float whole = R.sum_in + R.sum_out;
-    const float tail = !(whole > 0.f) ? -INFINITY : R.sum_in < R.sum_out ? log1pf(-R.sum_in / whole) : logf(R.sum_out / whole);
+    // (a sum outside S that is nothing beside the largest logit still has a logarithm)
+    const float tail = !(R.out.s > 0.f) ? -INFINITY : R.q_in < R.q_out ? log1pf(-R.q_in) : (ref_below(R.out.m, R.st.m, a.c) + log2f(R.out.s) - R.st.log2s) * LN2;
     double term = 0.0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -260,29 +278,15 @@ __device__ __forceinline__ void put_unit(void *grad, int64_t at, const float *g)
         __builtin_nontemporal_store(v, (Vec16Any4 *)((float *)grad + at));
     }
 }
-// q (a + b log2 q) of an element, q = 2^((x - m) c - log2 s)
-struct Slope {
-    float m, log2s, c, a, b;
-};
 template <bool ENT>
 __device__ __forceinline__ float slope_at(const Slope &k, float x) {
     const float t = fmaf(x - k.m, k.c, -k.log2s), q = __builtin_amdgcn_exp2f(t);
     return q * (ENT ? fmaf(k.b, fmaxf(t, -1e4f), k.a) : k.a);
 }
-__device__ __forceinline__ Slope slope(float m, float l, float c, float a, float b) {
-    // (nothing finite in the row: every q is 0)
-    return m == -INFINITY ? Slope{0.f, INFINITY, c, a, b} : Slope{m, l * LOG2E, c, a, b};
-}
 template <bool BF16>
 __device__ __forceinline__ void grad_zero(void *grad, int64_t at, int n, int nt) {
     for (int i = threadIdx.x; i < n; i += nt) put_elem<BF16>(grad, at + i, 0.f);
 }
-// What the gradients of a row with a teacher go by.
-struct DistillSlope {
-    Slope out;
-    float in_s, w;
-    int64_t at;
-};
 // a bit for each of the thread's elements of the go that are in S; room: the wave's
 template <int NT, int U>
 struct Hidden {
@@ -349,22 +353,18 @@ __device__ __forceinline__ void distill_put_go(const DistillArgs &a, const Row<B
     put_go<NT, G, false>(row, it, d.out, a.grad, d.at, raw);
     wave_sync();
     const int here = it * (NT / 64) + (threadIdx.x >> 6);
-    Slope in = d.out;
-    in.a = d.in_s;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s)
         if (E.where[s] == here) {
             const int i = 64 * s + lane_id();
-            put_elem<BF16>(a.grad, d.at + t.id[i], slope_at<false>(in, xs[s]) - d.w * t.sum[i]);
+            put_elem<BF16>(a.grad, d.at + t.id[i], slope_at<false>(d.in, xs[s]) - d.w * t.sum[i]);
         }
 }
 template <bool BF16>
 __device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, float x) {
     if (row.loose == 0 || threadIdx.x >= 64) return;
-    Slope in = d.out;
-    in.a = d.in_s;
     float g = slope_at<false>(d.out, x);
-    entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(in, x) - d.w * t.sum[i] : g; });
+    entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(d.in, x) - d.w * t.sum[i] : g; });
     if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
 }
 __device__ __forceinline__ void s_elems(const Teacher &t, float (&x)[SLOTS]) {
@@ -419,10 +419,10 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : NT == 64 ? 5 : BF16 ? (GRAD ? 
     go_keep(raw);
     if (row.loose > 0) sums_add1<false>(s, hide_loose(a, E, xl), a.c);
     s = block_sums<false, NT>(s, a.c, room);
-    const RowLoss R = row_loss(a, w, t, s);
+    const RowLoss R = row_loss(a, t, s);
     if (lead) loss_write(a, r, t, R);
     if (GRAD) {
-        const DistillSlope d = {slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride};
+        const DistillSlope d = loss_slope(a, w, t, R, r * a.grad_stride);
         float xs[SLOTS];
         s_elems(t, xs);
         distill_put_go<NT, G>(a, row, 0, E, t, d, raw, xs);
@@ -495,13 +495,13 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(
     }
     Sums s = sums_outside<BF16, GRAD, NT>(a, row, E, 0, goes, true);
     s = block_sums<false, NT>(s, a.c, room);
-    const RowLoss R = row_loss(a, w, t, s);
+    const RowLoss R = row_loss(a, t, s);
     if (lead) loss_write(a, r, t, R);
     Raw<BF16, U> raw = {};
     if (GRAD && goes > 0) go_request<NT, false>(row, 0, raw);
     float xs[SLOTS];
     s_elems(t, xs);
-    if (GRAD) grad_goes<NT>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, 0, goes, true, raw, xs);
+    if (GRAD) grad_goes<NT>(a, row, E, t, loss_slope(a, w, t, R, r * a.grad_stride), 0, goes, true, raw, xs);
 }
 
 // The sums of a row's parts, from float2 at `sums`, in every lane.
@@ -554,7 +554,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
     teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
     s = parts_sums(sums, a.parts, a.c);
     wave_sync();
-    loss_write(a, r, t, row_loss(a, 0.f, t, s));
+    loss_write(a, r, t, row_loss(a, t, s));
     parts_leave(marks, a.parts);
 }
 // The loss of rows whose parts are there.
@@ -578,7 +578,7 @@ __global__ __launch_bounds__(64) void distill_loss_kernel(DistillArgs a) {
     const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
     teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
     wave_sync();
-    loss_write(a, r, t, row_loss(a, 0.f, t, out));
+    loss_write(a, r, t, row_loss(a, t, out));
 }
 // The loss of rows whose parts are there, and the gradient of a part.
 template <bool BF16>
@@ -613,10 +613,10 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
     if (lead) teacher_probs(a, lse, G, xs, t);
     __syncthreads();
-    const RowLoss R = row_loss(a, w, t, out);
+    const RowLoss R = row_loss(a, t, out);
     if (lead && part == 0) loss_write(a, r, t, R);
     s_elems(t, xs);
-    grad_goes<NT>(a, row, E, t, DistillSlope{slope(R.st.m, R.st.l, a.c, R.out, 0.f), R.in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
+    grad_goes<NT>(a, row, E, t, loss_slope(a, w, t, R, r * a.grad_stride), first, end, part == 0, raw, xs);
 }
 
 // The gradient of a part of a row from what the loss has saved.
@@ -652,8 +652,8 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     }
     if (threadIdx.x < 64) teacher_probs(a, lse, G, xs, t);
     __syncthreads();
-    const float in_s = w * (t.P + t.rest), out = tail > -INFINITY ? in_s - w * t.rest * expf(-tail) : in_s;
-    grad_goes<NT>(a, row, E, t, DistillSlope{slope(m, l, a.c, out, 0.f), in_s, w, r * a.grad_stride}, first, end, part == 0, raw, xs);
+    const Slope out = slope(tail > -INFINITY ? m : -INFINITY, l + tail, a.c, w * (t.P * expf(tail) + t.rest * expm1f(tail)), 0.f);
+    grad_goes<NT>(a, row, E, t, DistillSlope{out, slope(m, l, a.c, w * (t.P + t.rest), 0.f), w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.

@@ -139,10 +139,12 @@ __device__ __forceinline__ float ref_off(float m, float c) {
     return plain_ref(M2) ? fmaf(-m, c, M2) : 0.f;
 }
 // how far, in powers of two, sums against `from` lie below those against `to`, to >= from
-__device__ __forceinline__ float ref_step(float from, float to, float c) {
+__device__ __forceinline__ float ref_below(float from, float to, float c) {
     const float a = from * c, b = to * c;
-    const float d = plain_ref(a) && plain_ref(b) ? a - b : from == to ? 0.f : (from - to) * c + (ref_off(from, c) - ref_off(to, c));
-    return fmaxf(d, -1e4f);  // (a sum of nothing, times any power, stays nothing)
+    return plain_ref(a) && plain_ref(b) ? a - b : from == to ? 0.f : (from - to) * c + (ref_off(from, c) - ref_off(to, c));
+}
+__device__ __forceinline__ float ref_step(float from, float to, float c) {
+    return fmaxf(ref_below(from, to, c), -1e4f);  // (a sum of nothing, times any power, stays nothing)
 }
 template <bool ENT>
 __device__ __forceinline__ void sums_move(Sums &a, float to, float c) {

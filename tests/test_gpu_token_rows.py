@@ -570,3 +570,50 @@ def test_graphs_that_share_a_workspace(n, m, V):
         for b, f in zip((one, two), first):
             for name in OUT:
                 assert torch.equal(b[name].view(torch.uint8), f[name].view(torch.uint8)), (i, name)
+
+
+@pytest.mark.parametrize("n, V, k", [(4, 4480, 1), (4, 4480, 9), (3, 1500, 3), (130, 40001, 5), (6, 50001, 2)])
+@pytest.mark.parametrize("noise", [0.0, 1e-3])
+def test_gradient_of_students_that_are_near_their_teacher(n, V, k, noise):
+    """Outside S the gradient is q_j / q_t (P q_t - p_t q_in), which is known to the digits of its two terms, however near to each other P and p_t + P q_in
+    may be: 8 delta times their sum, as for other gradients of size times delta."""
+    x, xd = rows(n, V, F32, n + V, offset=1, pad=1)
+    g = torch.Generator().manual_seed(k)
+    y = torch.log_softmax((x.double() / 2.0) + noise * torch.randn(n, V, generator=g, dtype=torch.float64), 1)
+    pick = torch.argsort(torch.rand(n, V, generator=g), 1)[:, :k]               # any entries, not the best: little in S
+    val, ids = y.gather(1, pick).float(), pick.int()
+    want = ref.distill(x, val, ids, None, None, 2.0, 1)
+    o = run_distill(xd, val, ids, None, None, 2.0, 1, None, True)
+    check_distill(o, want, F32, V)
+    lq = torch.log_softmax(x.double() / 2.0, 1)
+    P = torch.exp(val.double()).sum(1, keepdim=True)
+    q_in = torch.exp(lq.gather(1, pick)).sum(1, keepdim=True)
+    q = torch.exp(lq)
+    outside = torch.ones(n, V, dtype=torch.bool).scatter(1, pick, False)
+    tol = 8 * ref.delta(V) * q / (1 - q_in) * (P * (1 - q_in) + (1 - P) * q_in) + ref.HALF[F32] * want["grad"].abs() + ref.TINY
+    # (p_t is 1 - P, of fp32's digits: its own half step is one of delta's)
+    for name in ("grad", "again"):
+        ref.close(o[name].cpu()[outside], want["grad"][outside], tol[outside], name)
+    ref.close(o["tail"], want["tail"], 2 * ref.delta(V) * want["tail"].abs() * 1.5, "tail")    # relative: q_in is a sum of its own, and log(1 - q_in) is its size
+
+
+@pytest.mark.parametrize("n, V", [(3, 300), (3, 5000), (130, 40001), (6, 50001), (300, 33001)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("flags", [0, 1, 2])
+def test_students_that_are_as_good_as_certain(n, V, dtype, flags):
+    """What lies outside S is e^-500: nothing beside the largest logit in fp32, and yet its logarithm and its shares are there."""
+    k, T = 4, 0.4
+    x, _ = rows(n, V, dtype, V)
+    val, ids, lse = teacher(n, V, k, 5, short=False)
+    x = x.scatter(1, ids[:, :1].long(), 200.0)
+    some = torch.tensor([0, 1, n - 1])
+    want = ref.distill(x[some], val[some], ids[some], lse[some], None, T, flags)
+    assert torch.isfinite(want["loss"]).all() and (want["tail"] < -400).all()
+    o = run_distill(put(x), val, ids, lse, None, T, flags, None, True)
+    scale = 1 + 200.0 / T / 24                            # |x| / T up to 500
+    d = scale * ref.delta(V)
+    o = {name: v[some.to(DEV)] for name, v in o.items()}
+    ref.close(o["loss"], want["loss"], 2 * d * want["terms"], "loss")
+    ref.close(o["tail"], want["tail"], 2 * d * (1 + want["tail"].abs()), "tail")
+    for name in ("grad", "again"):
+        check_grad(o[name], want["grad"], scale * want["size"], dtype, V, (flags, name))
