@@ -18,13 +18,16 @@ namespace dt {
 
 // ---- the teacher's entries for a row ----
 #define SLOTS (DT_DISTILL_K_MAX / 64)  // entries of a lane
+struct TeacherHead {
+    float P, rest, in_m, in_s;         // the student's sum in S
+};
 struct Teacher {                       // the entries, as the first wave leaves them for all
     double p[DT_DISTILL_K_MAX], lp[DT_DISTILL_K_MAX];
     float sum[DT_DISTILL_K_MAX];       // p of all entries with the same id
     float x[DT_DISTILL_K_MAX];         // the student's logits
     int id[DT_DISTILL_K_MAX];          // -1: none
     int found[512];                    // an entry for a hash of its id
-    float P, rest, in_m, in_s;         // the student's sum in S
+    TeacherHead head;
 };
 struct Entries {  // of a lane: where they are worked on
     int where[SLOTS];   // go * waves + wave, -1: a loose element, -2: none
@@ -61,7 +64,7 @@ __device__ __forceinline__ void entries_place(const DistillArgs &a, const Row<BF
         E.which[s] = (p.thread & 63) | p.elem << 6;
     }
 }
-// f(lane, element, entry) for the entries at `where` (uniform): one after the other, the same for all lanes
+// f(lane, slot, lane of the entry) for the entries at `where` (uniform), of `lane`: one after the other, the same for all lanes
 template <class F>
 __device__ __forceinline__ void entries_at(const DistillArgs &a, const Entries &E, int where, F f) {
 #pragma unroll
@@ -69,7 +72,7 @@ __device__ __forceinline__ void entries_at(const DistillArgs &a, const Entries &
         if (s && a.k <= 64 * s) break;  // uniform
         for (u64 b = ballot(E.where[s] == where); b; b &= b - 1) {
             const int i = __builtin_ctzll(b), w = __builtin_amdgcn_readlane(E.which[s], i);
-            f(w & 63, w >> 6, 64 * s + i);
+            f(w & 63, s, i);
         }
     }
 }
@@ -182,10 +185,7 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
         if (first[s]) sums_add1<false>(in, x[s], a.c);
     wave_sums<false>(in, a.c);
     if (lane == 0) {
-        t.P = (float)P;
-        t.rest = (a.flags & DT_DISTILL_TAIL) ? (float)fmax(0.0, 1.0 - P) : 0.f;
-        t.in_m = in.m;
-        t.in_s = in.s;
+        t.head = TeacherHead{(float)P, (a.flags & DT_DISTILL_TAIL) ? (float)fmax(0.0, 1.0 - P) : 0.f, in.m, in.s};
     }
 }
 
@@ -212,7 +212,7 @@ struct RowLoss {
     float q_in, q_out;  // of the student
     Sums out;
 };
-__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const Teacher &t, const Sums &out) {
+__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const TeacherHead &t, const Sums &out) {
     Sums in = {t.in_m, t.in_s, 0.f}, o = out;
     const float m = fmaxf(in.m, out.m);
     sums_move<false>(in, m, a.c);
@@ -225,14 +225,25 @@ __device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const Teacher 
     R.out = out;
     return R;
 }
-__device__ __forceinline__ DistillSlope loss_slope(const DistillArgs &a, float w, const Teacher &t, const RowLoss &R, int64_t at) {
+__device__ __forceinline__ DistillSlope loss_slope(const DistillArgs &a, float w, const TeacherHead &t, const RowLoss &R, int64_t at) {
     const RowStat o = row_stat(R.out.m, R.out.s, a.c);
     return DistillSlope{slope(o.m, o.l, a.c, w * (t.P * R.q_out - t.rest * R.q_in), 0.f), slope(R.st.m, R.st.l, a.c, w * (t.P + t.rest), 0.f), w, at};
 }
+// (a sum outside S that is nothing beside the largest logit still has a logarithm)
+__device__ __forceinline__ float log_outside(const DistillArgs &a, const RowLoss &R) {
+    return !(R.out.s > 0.f) ? -INFINITY : R.q_in < R.q_out ? log1pf(-R.q_in) : (ref_below(R.out.m, R.st.m, a.c) + log2f(R.out.s) - R.st.log2s) * LN2;
+}
+// one lane; in: the loss of the entries
+__device__ __forceinline__ void loss_store(const DistillArgs &a, int64_t r, const TeacherHead &t, const RowLoss &R, double in) {
+    const float tail = log_outside(a, R);
+    if (t.rest > 0.f) in += (double)t.rest * ((double)logf(t.rest) - (double)tail);
+    a.loss[r] = (float)in;
+    a.stats[2 * r] = R.st.m;
+    a.stats[2 * r + 1] = R.st.l;
+    a.tail[r] = tail;
+}
 // by the first wave
 __device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, const Teacher &t, const RowLoss &R) {
-    // (a sum outside S that is nothing beside the largest logit still has a logarithm)
-    const float tail = !(R.out.s > 0.f) ? -INFINITY : R.q_in < R.q_out ? log1pf(-R.q_in) : (ref_below(R.out.m, R.st.m, a.c) + log2f(R.out.s) - R.st.log2s) * LN2;
     double term = 0.0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -240,14 +251,22 @@ __device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, cons
         const double p = t.p[i];
         if (p > 0.0) term += p * (t.lp[i] - (double)log_prob(t.x[i], R.st, a.c));
     }
-    if (lane_id() == 0 && t.rest > 0.f) term += (double)t.rest * ((double)logf(t.rest) - (double)tail);
     term = wave_sum_f64(term);
-    if (lane_id() == 0) {
-        a.loss[r] = (float)term;
-        a.stats[2 * r] = R.st.m;
-        a.stats[2 * r + 1] = R.st.l;
-        a.tail[r] = tail;
+    if (lane_id() == 0) loss_store(a, r, t.head, R, term);
+}
+// Where the row's sums come together elsewhere: sum p_i (log p_i - (x_i - m) / T), m the largest logit in S, to which the log-probability of m is to be added P times.
+__device__ __forceinline__ double loss_in(const DistillArgs &a, const Teacher &t) {
+    double term = 0.0;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int i = 64 * s + lane_id();
+        const double p = t.p[i];
+        if (p > 0.0) term += p * (t.lp[i] - (t.head.in_m > -INFINITY ? ((double)t.x[i] - (double)t.head.in_m) * (double)(a.c * LN2) : -INFINITY));
     }
+    return wave_sum_f64(term);
+}
+__device__ __forceinline__ double loss_of(const DistillArgs &a, const TeacherHead &t, double in, const RowLoss &R) {
+    return t.P > 0.f && t.in_m > -INFINITY ? in - (double)t.P * (double)log_prob(t.in_m, R.st, a.c) : in;
 }
 __device__ __forceinline__ void row_loss_none(const DistillArgs &a, int64_t r) {
     if (threadIdx.x == 0) a.loss[r] = a.stats[2 * r] = a.stats[2 * r + 1] = a.tail[r] = 0.f;
@@ -345,26 +364,37 @@ __device__ __forceinline__ void put_go(const Row<BF16> &row, int it, const Slope
         }
     }
 }
+// A lane's entries as the gradient needs them: from what the first wave has left, or as the launch before has.
+struct OwnLeft {
+    const Teacher &t;
+    __device__ __forceinline__ int id(int s) const { return t.id[64 * s + lane_id()]; }
+    __device__ __forceinline__ float sum(int s) const { return t.sum[64 * s + lane_id()]; }
+    __device__ __forceinline__ float sum_of(int s, int lane) const { return t.sum[64 * s + lane]; }
+};
+struct OwnLoaded {
+    int ids[SLOTS];
+    float sums[SLOTS];
+    __device__ __forceinline__ int id(int s) const { return ids[s]; }
+    __device__ __forceinline__ float sum(int s) const { return sums[s]; }
+    __device__ __forceinline__ float sum_of(int s, int lane) const { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sums[s]), lane)); }
+};
 // Of a row with a teacher: all as if outside S, then those in S, from the lanes that have them as entries; xs: their logits.  (The stores of a wave to
 // one address take effect in the order of its instructions.)
-template <int NT, int G, bool BF16, int U>
-__device__ __forceinline__ void distill_put_go(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Teacher &t, const DistillSlope &d,
+template <int NT, int G, bool BF16, int U, class Own>
+__device__ __forceinline__ void distill_put_go(const DistillArgs &a, const Row<BF16> &row, int it, const Entries &E, const Own &own, const DistillSlope &d,
                                                const Raw<BF16, U> &raw, const float (&xs)[SLOTS]) {
     put_go<NT, G, false>(row, it, d.out, a.grad, d.at, raw);
     wave_sync();
     const int here = it * (NT / 64) + (threadIdx.x >> 6);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s)
-        if (E.where[s] == here) {
-            const int i = 64 * s + lane_id();
-            put_elem<BF16>(a.grad, d.at + t.id[i], slope_at<false>(d.in, xs[s]) - d.w * t.sum[i]);
-        }
+        if (E.where[s] == here) put_elem<BF16>(a.grad, d.at + own.id(s), slope_at<false>(d.in, xs[s]) - d.w * own.sum(s));
 }
-template <bool BF16>
-__device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, float x) {
+template <bool BF16, class Own>
+__device__ __forceinline__ void distill_grad_loose(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Own &own, const DistillSlope &d, float x) {
     if (row.loose == 0 || threadIdx.x >= 64) return;
     float g = slope_at<false>(d.out, x);
-    entries_at(a, E, -1, [&](int lane, int, int i) { g = lane_id() == lane ? slope_at<false>(d.in, x) - d.w * t.sum[i] : g; });
+    entries_at(a, E, -1, [&](int lane, int s, int i) { g = lane_id() == lane ? slope_at<false>(d.in, x) - d.w * own.sum_of(s, i) : g; });
     if ((int)threadIdx.x < row.loose) put_elem<BF16>(a.grad, d.at + row.loose_at(threadIdx.x), g);
 }
 __device__ __forceinline__ void s_elems(const Teacher &t, float (&x)[SLOTS]) {
@@ -419,14 +449,14 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 4 : NT == 64 ? 5 : BF16 ? (GRAD ? 
     go_keep(raw);
     if (row.loose > 0) sums_add1<false>(s, hide_loose(a, E, xl), a.c);
     s = block_sums<false, NT>(s, a.c, room);
-    const RowLoss R = row_loss(a, t, s);
+    const RowLoss R = row_loss(a, t.head, s);
     if (lead) loss_write(a, r, t, R);
     if (GRAD) {
-        const DistillSlope d = loss_slope(a, w, t, R, r * a.grad_stride);
+        const DistillSlope d = loss_slope(a, w, t.head, R, r * a.grad_stride);
         float xs[SLOTS];
         s_elems(t, xs);
-        distill_put_go<NT, G>(a, row, 0, E, t, d, raw, xs);
-        distill_grad_loose(a, row, E, t, d, xl);
+        distill_put_go<NT, G>(a, row, 0, E, OwnLeft{t}, d, raw, xs);
+        distill_grad_loose(a, row, E, OwnLeft{t}, d, xl);
     }
 }
 
@@ -452,18 +482,18 @@ __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF1
     }
     return s;
 }
-template <int NT, bool BF16>
-__device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Teacher &t, const DistillSlope &d, int first, int end,
+template <int NT, bool BF16, class Own>
+__device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Own &own, const DistillSlope &d, int first, int end,
                                           bool loose, Raw<BF16, STREAM_U> raw, const float (&xs)[SLOTS]) {
     constexpr int U = STREAM_U;
     for (int it = first; it < end; ++it) {
         if (it > first) go_request<NT, false>(row, it, raw);
         go_keep(raw);
-        distill_put_go<NT, 1>(a, row, it, E, t, d, raw, xs);
+        distill_put_go<NT, 1>(a, row, it, E, own, d, raw, xs);
     }
     if (loose) {
         const float xl = (int)threadIdx.x < row.loose ? row.at(row.loose_at(threadIdx.x)) : -INFINITY;
-        distill_grad_loose(a, row, E, t, d, xl);
+        distill_grad_loose(a, row, E, own, d, xl);
     }
 }
 
@@ -495,13 +525,13 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(
     }
     Sums s = sums_outside<BF16, GRAD, NT>(a, row, E, 0, goes, true);
     s = block_sums<false, NT>(s, a.c, room);
-    const RowLoss R = row_loss(a, t, s);
+    const RowLoss R = row_loss(a, t.head, s);
     if (lead) loss_write(a, r, t, R);
     Raw<BF16, U> raw = {};
     if (GRAD && goes > 0) go_request<NT, false>(row, 0, raw);
     float xs[SLOTS];
     s_elems(t, xs);
-    if (GRAD) grad_goes<NT>(a, row, E, t, loss_slope(a, w, t, R, r * a.grad_stride), 0, goes, true, raw, xs);
+    if (GRAD) grad_goes<NT>(a, row, E, OwnLeft{t}, loss_slope(a, w, t.head, R, r * a.grad_stride), 0, goes, true, raw, xs);
 }
 
 // The sums of a row's parts, from float2 at `sums`, in every lane.
@@ -515,14 +545,35 @@ __device__ __forceinline__ Sums parts_sums(u64 *sums, int parts, float c) {
     wave_sums<false>(s, c);
     return s;
 }
-// Sums outside S of a part of a row.  LAST: who is last of a row's says its loss.  Else the next launch does, and finds the elements of S as the first part has left
-// them, since it may write their gradients over them.
+// What is left of a row's teacher for those who join its parts: three words at `at`, put by one wave.
+struct RowHead {
+    TeacherHead t;
+    double in;
+};
+__device__ __forceinline__ void head_put(u64 *at, const Teacher &t, double in) {
+    if (lane_id() != 0) return;
+    put_agent(at, (u64)__float_as_uint(t.head.rest) << 32 | __float_as_uint(t.head.P));
+    put_agent(at + 1, (u64)__float_as_uint(t.head.in_s) << 32 | __float_as_uint(t.head.in_m));
+    put_agent(at + 2, (u64)__double_as_longlong(in));
+}
+__device__ __forceinline__ RowHead head_get(u64 *at) {
+    const u64 p = get_agent(at), q = get_agent(at + 1), in = get_agent(at + 2);
+    return RowHead{{__uint_as_float((u32)p), __uint_as_float((u32)(p >> 32)), __uint_as_float((u32)q), __uint_as_float((u32)(q >> 32))},
+                   __longlong_as_double((long long)in)};
+}
+// Sums outside S of a part of a row, after workgroups that have the rows' teachers: a multiple of the XCDs' number, so that the next launch finds a part in
+// the L2 where it was read.  LAST: who is last of a row's says its loss.  Else the next launch does, and finds the elements of S as they are left
+// here, since it may write their gradients over them.
+__host__ __device__ __forceinline__ u32 teacher_groups(int64_t n) { return (u32)(n + 7) & ~7u; }
 template <bool BF16, bool LAST>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Sums room[NT / 64];
     __shared__ Teacher t;
-    const RowPart rp = row_part(a.parts);
+    const u32 teachers = teacher_groups(a.n);
+    const bool has_teacher = blockIdx.x < teachers;
+    if (has_teacher && blockIdx.x >= a.n) return;
+    const RowPart rp = has_teacher ? RowPart{blockIdx.x, a.parts} : row_part(blockIdx.x - teachers, a.parts);
     const int64_t r = rp.row;
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
@@ -531,61 +582,57 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
         return;
     }
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
+    u64 *const sums = (u64 *)a.ws + r * a.parts, *const head = (u64 *)a.ws + a.n * a.parts + 3 * r;
     Given G;
     Entries E;
     entries_load(a, tr, G);
     entries_place<NT, U>(a, row, G, E);
-    float xs[SLOTS];
-    if (!LAST && part == 0 && threadIdx.x < 64) {
+    if (!has_teacher) {
+        Sums s = sums_outside<BF16, !LAST, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
+        s = block_sums<false, NT>(s, a.c, room);
+        if (threadIdx.x >= 64) return;
+        if (threadIdx.x == 0) put_agent(sums + part, (u64)__float_as_uint(s.s) << 32 | __float_as_uint(s.m));
+    } else {
+        if (threadIdx.x >= 64) return;
+        float xs[SLOTS];
         s_elems<BF16>(row, G, xs);
+        teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
+        wave_sync();
+        if (!LAST && a.grad) {
+            float2 *const entries = a.entries + r * a.k;
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s)
-            if (64 * s + lane_id() < a.k) a.s_elems[r * a.k + 64 * s + lane_id()] = xs[s];
+            for (int s = 0; s < SLOTS; ++s) {
+                const int i = 64 * s + lane_id();
+                if (i < a.k) entries[i] = make_float2(xs[s], t.sum[i]);
+            }
+        }
+        head_put(head, t, loss_in(a, t));
     }
-    Sums s = sums_outside<BF16, !LAST, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
-    s = block_sums<false, NT>(s, a.c, room);
-    if (threadIdx.x >= 64) return;
-    u64 *const sums = (u64 *)a.ws + r * a.parts;
-    if (threadIdx.x == 0) put_agent(sums + part, (u64)__float_as_uint(s.s) << 32 | __float_as_uint(s.m));
     if (!LAST) return;
-    u64 *const marks = (u64 *)a.ws + a.n * a.parts + r * a.parts;
-    if (!part_arrive(marks, part, a.parts, a.tag)) return;
-    s_elems<BF16>(row, G, xs);
-    teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
-    s = parts_sums(sums, a.parts, a.c);
-    wave_sync();
-    loss_write(a, r, t, row_loss(a, t, s));
-    parts_leave(marks, a.parts);
+    u64 *const marks = (u64 *)a.ws + a.n * (a.parts + 3) + r * (a.parts + 1);
+    if (!part_arrive(marks, part, a.parts + 1, a.tag)) return;
+    const RowHead h = head_get(head);
+    const RowLoss R = row_loss(a, h.t, parts_sums(sums, a.parts, a.c));
+    if (lane_id() == 0) loss_store(a, r, h.t, R, loss_of(a, h.t, h.in, R));
+    parts_leave(marks, a.parts + 1);
 }
 // The loss of rows whose parts are there.
 __global__ __launch_bounds__(64) void distill_loss_kernel(DistillArgs a) {
-    __shared__ Teacher t;
     const int64_t r = blockIdx.x;
-    const int64_t tr = teacher_row(a, r);
-    if (tr < 0) {
+    const RowHead h = head_get((u64 *)a.ws + a.n * a.parts + 3 * r);
+    const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
+    if (teacher_row(a, r) < 0) {
         row_loss_none(a, r);
         return;
     }
-    Given G;
-    entries_load(a, tr, G);
-    float xs[SLOTS];
-#pragma unroll
-    for (int s = 0; s < SLOTS; ++s) {
-        const int i = 64 * s + lane_id();
-        xs[s] = i < a.k ? a.s_elems[r * a.k + i] : -INFINITY;
-        if (!(G.id[s] >= 0 && G.id[s] < a.V && G.val[s] > -INFINITY)) G.id[s] = -1;
-    }
-    const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
-    teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
-    wave_sync();
-    loss_write(a, r, t, row_loss(a, t, out));
+    const RowLoss R = row_loss(a, h.t, out);
+    if (lane_id() == 0) loss_store(a, r, h.t, R, loss_of(a, h.t, h.in, R));
 }
 // The loss of rows whose parts are there, and the gradient of a part.
 template <bool BF16>
 __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
-    __shared__ Teacher t;
-    const RowPart rp = row_part(a.parts);
+    const RowPart rp = row_part(blockIdx.x, a.parts);
     const int64_t r = rp.row;
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
@@ -597,26 +644,28 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
         grad_zero<BF16>(a.grad, r * a.grad_stride + from, to - from, NT);
         return;
     }
-    const bool lead = threadIdx.x < 64;
-    const float lse = a.teacher_lse ? a.teacher_lse[tr] : 0.f, w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
+    const float w = (a.grad_loss ? a.grad_loss[r] : 1.f) * a.inv_t;
     Given G;
     Entries E;
     entries_load(a, tr, G);
+    OwnLoaded own;
     float xs[SLOTS];
-    if (lead) {
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) xs[s] = 64 * s + lane_id() < a.k ? a.s_elems[r * a.k + 64 * s + lane_id()] : -INFINITY;
+    for (int s = 0; s < SLOTS; ++s) {
+        const float2 e = 64 * s + lane_id() < a.k ? a.entries[r * a.k + 64 * s + lane_id()] : make_float2(0.f, 0.f);
+        xs[s] = e.x;
+        own.sums[s] = e.y;
     }
+    const RowHead h = head_get((u64 *)a.ws + a.n * a.parts + 3 * r);
     Raw<BF16, U> raw = {};
     if (first < end) go_request<NT, false>(row, first, raw);
-    entries_place<NT, U>(a, row, G, E);
     const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
-    if (lead) teacher_probs(a, lse, G, xs, t);
-    __syncthreads();
-    const RowLoss R = row_loss(a, t, out);
-    if (lead && part == 0) loss_write(a, r, t, R);
-    s_elems(t, xs);
-    grad_goes<NT>(a, row, E, t, loss_slope(a, w, t, R, r * a.grad_stride), first, end, part == 0, raw, xs);
+    entries_place<NT, U>(a, row, G, E);
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) own.ids[s] = G.id[s];
+    const RowLoss R = row_loss(a, h.t, out);
+    if (part == 0 && threadIdx.x == 0) loss_store(a, r, h.t, R, loss_of(a, h.t, h.in, R));
+    grad_goes<NT>(a, row, E, own, loss_slope(a, w, h.t, R, r * a.grad_stride), first, end, part == 0, raw, xs);
 }
 
 // The gradient of a part of a row from what the loss has saved.
@@ -624,7 +673,7 @@ template <bool BF16>
 __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
-    const RowPart rp = row_part(a.parts);
+    const RowPart rp = row_part(blockIdx.x, a.parts);
     const int64_t r = rp.row;
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
@@ -652,8 +701,8 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     }
     if (threadIdx.x < 64) teacher_probs(a, lse, G, xs, t);
     __syncthreads();
-    const Slope out = slope(tail > -INFINITY ? m : -INFINITY, l + tail, a.c, w * (t.P * expf(tail) + t.rest * expm1f(tail)), 0.f);
-    grad_goes<NT>(a, row, E, t, DistillSlope{out, slope(m, l, a.c, w * (t.P + t.rest), 0.f), w, r * a.grad_stride}, first, end, part == 0, raw, xs);
+    const Slope out = slope(tail > -INFINITY ? m : -INFINITY, l + tail, a.c, w * (t.head.P * expf(tail) + t.head.rest * expm1f(tail)), 0.f);
+    grad_goes<NT>(a, row, E, OwnLeft{t}, DistillSlope{out, slope(m, l, a.c, w * (t.head.P + t.head.rest), 0.f), w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.
@@ -661,7 +710,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
 template <bool BF16, bool ENT>
 __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
-    const RowPart rp = row_part(a.parts);
+    const RowPart rp = row_part(blockIdx.x, a.parts);
     const int64_t r = rp.row, at = r * a.grad_stride;
     const int part = rp.part, first = part * a.part_goes;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
@@ -725,7 +774,7 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
             else if constexpr (BF16) held(Held<1024, 16>());
         }
     } else if (cut == PARTS) {
-        const dim3 grid((u32)(a.n * a.parts));
+        const dim3 grid((u32)(a.n * a.parts) + teacher_groups(a.n));
         if (!GRAD && a.n < PARTS_ROWS) {
             launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
             return hipGetLastError();
@@ -733,7 +782,7 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
         launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        if constexpr (GRAD) launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, grid, dim3(STREAM_NT), 0, a);
+        if constexpr (GRAD) launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
         else launch_kernel(KID_DISTILL_JOIN, st, distill_loss_kernel, dim3((u32)a.n), dim3(64), 0, a);
     } else if (cut == WIDE) {
         if constexpr (!GRAD)
@@ -744,15 +793,16 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Sums of the parts, then their marks or, with the gradient, the elements of S: as many as parts can be, as for logprob_workspace.
+// Sums of the parts, three words of the teacher, then marks or, with the gradient, the elements of S: as many as parts can be, as for logprob_workspace.
 size_t distill_workspace(int64_t n, int V) {
     const size_t goes = row_goes(V);
-    return (size_t)std::min(n, MEET_ROWS - 1) * (goes * 8 + std::max<size_t>(goes * 8, DT_DISTILL_K_MAX * sizeof(float)));
+    return (size_t)std::min(n, MEET_ROWS - 1) * (goes * 8 + 24 + std::max<size_t>(goes * 8 + 8, DT_DISTILL_K_MAX * sizeof(float2)));
 }
 hipError_t distill_launch(DistillArgs a, hipStream_t st) {
     a.part_goes = part_goes(a.n, a.V);
+    if (row_parts(a.V, a.part_goes) == 64) a.part_goes *= 2;  // (a mark to a lane, and the teacher's)
     a.parts = row_parts(a.V, a.part_goes);
-    a.s_elems = (float *)((u64 *)a.ws + a.n * a.parts);
+    a.entries = (float2 *)((u64 *)a.ws + a.n * (a.parts + 3));
     a.tag = launch_tag();
     if (a.dtype == DT_BF16) return a.grad ? launch_distill<true, true>(a, st) : launch_distill<true, false>(a, st);
     return a.grad ? launch_distill<false, true>(a, st) : launch_distill<false, false>(a, st);

@@ -237,7 +237,7 @@ struct DistillArgs {
     float *loss, *stats, *tail;
     void *grad;                              // or null
     void *ws;                                // sums of the parts of rows, then
-    float *s_elems;                          // [n, k] the student's logits of the teacher's tokens
+    float2 *entries;                         // [n, k] the student's logits of the teacher's tokens, the sums of their p
     unsigned long long tag;                  // of the launch; this and the next are set by it
     int parts, part_goes;
 };

@@ -397,7 +397,7 @@ __global__ __launch_bounds__(NT, ASK ? 4 : 8) void logprob_stream_kernel(Logprob
 template <bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(STREAM_NT, 8) void logprob_parts_kernel(LogprobArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U, WORDS = NT / 4;  // words of a go
-    const RowPart rp = row_part(a.parts);
+    const RowPart rp = row_part(blockIdx.x, a.parts);
     const int64_t e = rp.row;
     const int part = rp.part, tid = threadIdx.x;
     __shared__ Sums s_sums[NT / 64];

@@ -339,9 +339,9 @@ struct RowPart {
     int64_t row;
     int part;
 };
-__device__ __forceinline__ RowPart row_part(int parts) {
-    const u32 r = parts == 1 ? blockIdx.x : blockIdx.x / (u32)parts;
-    return RowPart{(int64_t)r, (int)(blockIdx.x - r * (u32)parts)};
+__device__ __forceinline__ RowPart row_part(u32 i, int parts) {
+    const u32 r = parts == 1 ? i : i / (u32)parts;
+    return RowPart{(int64_t)r, (int)(i - r * (u32)parts)};
 }
 
 }  // namespace dt
