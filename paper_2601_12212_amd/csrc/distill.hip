@@ -534,38 +534,30 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(
     if (GRAD) grad_goes<NT>(a, row, E, OwnLeft{t}, loss_slope(a, w, t.head, R, r * a.grad_stride), 0, goes, true, raw, xs);
 }
 
-// The sums of a row's parts, from float2 at `sums`, in every lane.
-__device__ __forceinline__ Sums parts_sums(u64 *sums, int parts, float c) {
-    Sums s = {-INFINITY, 0.f, 0.f};
-    if (lane_id() < parts) {
-        const u64 p = get_agent(sums + lane_id());
-        s.m = __uint_as_float((u32)p);
-        s.s = __uint_as_float((u32)(p >> 32));
-    }
-    wave_sums<false>(s, c);
-    return s;
-}
-// What is left of a row's teacher for those who join its parts: three words at `at`, put by one wave.
+// What is left of a row's teacher for those who join its parts.
 struct RowHead {
     TeacherHead t;
     double in;
 };
-__device__ __forceinline__ void head_put(u64 *at, const Teacher &t, double in) {
-    if (lane_id() != 0) return;
-    put_agent(at, (u64)__float_as_uint(t.head.rest) << 32 | __float_as_uint(t.head.P));
-    put_agent(at + 1, (u64)__float_as_uint(t.head.in_s) << 32 | __float_as_uint(t.head.in_m));
-    put_agent(at + 2, (u64)__double_as_longlong(in));
+// the workspace: sums of the parts (largest logit, sum), heads, entries
+__device__ __forceinline__ float2 *row_sums(const DistillArgs &a, int64_t r) { return (float2 *)a.ws + r * a.parts; }
+__device__ __forceinline__ RowHead *row_heads(const DistillArgs &a) { return (RowHead *)((float2 *)a.ws + a.n * a.parts); }
+// of all parts, in every lane
+__device__ __forceinline__ Sums parts_sums(const DistillArgs &a, int64_t r) {
+    Sums s = {-INFINITY, 0.f, 0.f};
+    if (lane_id() < a.parts) {
+        const float2 p = row_sums(a, r)[lane_id()];
+        s.m = p.x;
+        s.s = p.y;
+    }
+    wave_sums<false>(s, a.c);
+    return s;
 }
-__device__ __forceinline__ RowHead head_get(u64 *at) {
-    const u64 p = get_agent(at), q = get_agent(at + 1), in = get_agent(at + 2);
-    return RowHead{{__uint_as_float((u32)p), __uint_as_float((u32)(p >> 32)), __uint_as_float((u32)q), __uint_as_float((u32)(q >> 32))},
-                   __longlong_as_double((long long)in)};
-}
-// Sums outside S of a part of a row, after workgroups that have the rows' teachers: a multiple of the XCDs' number, so that the next launch finds a part in
-// the L2 where it was read.  LAST: who is last of a row's says its loss.  Else the next launch does, and finds the elements of S as they are left
-// here, since it may write their gradients over them.
 __host__ __device__ __forceinline__ u32 teacher_groups(int64_t n) { return (u32)(n + 7) & ~7u; }
-template <bool BF16, bool LAST>
+// Sums outside S of a part of a row, after workgroups that have the rows' teachers: a multiple of the XCDs' number, so that the next launch finds a part in
+// the L2 where it was read, and the elements of S as they are left here, since it may write their gradients over them.  (The loss by the part that arrives last,
+// in one launch: 127 fp32 rows of 128,256 entries 16.7 us, 15.2 so, 30 bf16 rows 8.0 and 6.8.)
+template <bool BF16, bool GRAD>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Sums room[NT / 64];
@@ -577,28 +569,23 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
     const int64_t r = rp.row;
     const int part = rp.part, first = part * a.part_goes;
     const int64_t tr = teacher_row(a, r);
-    if (tr < 0) {
-        if (LAST && part == 0) row_loss_none(a, r);
-        return;
-    }
+    if (tr < 0) return;
     const Row<BF16> row(a.logits, r * a.row_stride, a.V);
-    u64 *const sums = (u64 *)a.ws + r * a.parts, *const head = (u64 *)a.ws + a.n * a.parts + 3 * r;
     Given G;
     Entries E;
     entries_load(a, tr, G);
     entries_place<NT, U>(a, row, G, E);
     if (!has_teacher) {
-        Sums s = sums_outside<BF16, !LAST, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
+        Sums s = sums_outside<BF16, GRAD, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
         s = block_sums<false, NT>(s, a.c, room);
-        if (threadIdx.x >= 64) return;
-        if (threadIdx.x == 0) put_agent(sums + part, (u64)__float_as_uint(s.s) << 32 | __float_as_uint(s.m));
+        if (threadIdx.x == 0) row_sums(a, r)[part] = make_float2(s.m, s.s);
     } else {
         if (threadIdx.x >= 64) return;
         float xs[SLOTS];
         s_elems<BF16>(row, G, xs);
         teacher_probs(a, a.teacher_lse ? a.teacher_lse[tr] : 0.f, G, xs, t);
         wave_sync();
-        if (!LAST && a.grad) {
+        if (GRAD) {
             float2 *const entries = a.entries + r * a.k;
 #pragma unroll
             for (int s = 0; s < SLOTS; ++s) {
@@ -606,21 +593,15 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
                 if (i < a.k) entries[i] = make_float2(xs[s], t.sum[i]);
             }
         }
-        head_put(head, t, loss_in(a, t));
+        const double in = loss_in(a, t);
+        if (lane_id() == 0) row_heads(a)[r] = RowHead{t.head, in};
     }
-    if (!LAST) return;
-    u64 *const marks = (u64 *)a.ws + a.n * (a.parts + 3) + r * (a.parts + 1);
-    if (!part_arrive(marks, part, a.parts + 1, a.tag)) return;
-    const RowHead h = head_get(head);
-    const RowLoss R = row_loss(a, h.t, parts_sums(sums, a.parts, a.c));
-    if (lane_id() == 0) loss_store(a, r, h.t, R, loss_of(a, h.t, h.in, R));
-    parts_leave(marks, a.parts + 1);
 }
 // The loss of rows whose parts are there.
 __global__ __launch_bounds__(64) void distill_loss_kernel(DistillArgs a) {
     const int64_t r = blockIdx.x;
-    const RowHead h = head_get((u64 *)a.ws + a.n * a.parts + 3 * r);
-    const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
+    const RowHead h = row_heads(a)[r];
+    const Sums out = parts_sums(a, r);
     if (teacher_row(a, r) < 0) {
         row_loss_none(a, r);
         return;
@@ -656,10 +637,10 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
         xs[s] = e.x;
         own.sums[s] = e.y;
     }
-    const RowHead h = head_get((u64 *)a.ws + a.n * a.parts + 3 * r);
+    const RowHead h = row_heads(a)[r];
     Raw<BF16, U> raw = {};
     if (first < end) go_request<NT, false>(row, first, raw);
-    const Sums out = parts_sums((u64 *)a.ws + r * a.parts, a.parts, a.c);
+    const Sums out = parts_sums(a, r);
     entries_place<NT, U>(a, row, G, E);
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) own.ids[s] = G.id[s];
@@ -753,8 +734,8 @@ static Cut grad_cut(int64_t n, int V, bool bf16) {
     if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= MEET_ROWS && launch_holds(n, 1024)))) return HELD;
     return n < MEET_ROWS ? PARTS : WHOLE;
 }
-// The loss alone: as log-probabilities, but little more than one row to a compute unit in parts that a second launch joins (300 rows of 50,001 fp32 entries 16.7 us;
-// in one launch, whose parts wait for what they leave to arrive, 19.9, wide 20.5, whole 20.9), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
+// The loss alone: as log-probabilities (200 rows of 50,001 bf16 entries wide 9.5 us, in parts 10.5), but little more than one row to a compute unit in parts (300 rows of
+// 50,001 fp32 entries 15.2 us, wide 20.5, whole 20.9), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
 static Cut loss_cut(int64_t n, int V, bool bf16) {
     const Cut c = rows_cut(n, V, bf16, true);
     return c == AHEAD || (c == WIDE && n > CUS) ? n < MEET_ROWS ? PARTS : c == WIDE ? WIDE : WHOLE : c;
@@ -775,11 +756,7 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
         }
     } else if (cut == PARTS) {
         const dim3 grid((u32)(a.n * a.parts) + teacher_groups(a.n));
-        if (!GRAD && a.n < PARTS_ROWS) {
-            launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
-            return hipGetLastError();
-        }
-        launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
+        launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, GRAD>, grid, dim3(STREAM_NT), 0, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if constexpr (GRAD) launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
@@ -793,17 +770,14 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Sums of the parts, three words of the teacher, then marks or, with the gradient, the elements of S: as many as parts can be, as for logprob_workspace.
+// As many as parts can be, as for logprob_workspace.
 size_t distill_workspace(int64_t n, int V) {
-    const size_t goes = row_goes(V);
-    return (size_t)std::min(n, MEET_ROWS - 1) * (goes * 8 + 24 + std::max<size_t>(goes * 8 + 8, DT_DISTILL_K_MAX * sizeof(float2)));
+    return (size_t)std::min(n, MEET_ROWS - 1) * (row_goes(V) * sizeof(float2) + sizeof(RowHead) + DT_DISTILL_K_MAX * sizeof(float2));
 }
 hipError_t distill_launch(DistillArgs a, hipStream_t st) {
     a.part_goes = part_goes(a.n, a.V);
-    if (row_parts(a.V, a.part_goes) == 64) a.part_goes *= 2;  // (a mark to a lane, and the teacher's)
     a.parts = row_parts(a.V, a.part_goes);
-    a.entries = (float2 *)((u64 *)a.ws + a.n * (a.parts + 3));
-    a.tag = launch_tag();
+    a.entries = (float2 *)((RowHead *)((float2 *)a.ws + a.n * a.parts) + a.n);
     if (a.dtype == DT_BF16) return a.grad ? launch_distill<true, true>(a, st) : launch_distill<true, false>(a, st);
     return a.grad ? launch_distill<false, true>(a, st) : launch_distill<false, false>(a, st);
 }

@@ -238,7 +238,6 @@ struct DistillArgs {
     void *grad;                              // or null
     void *ws;                                // sums of the parts of rows, then
     float2 *entries;                         // [n, k] the student's logits of the teacher's tokens, the sums of their p
-    unsigned long long tag;                  // of the launch; this and the next are set by it
     int parts, part_goes;
 };
 size_t distill_workspace(int64_t n, int V);
