@@ -482,12 +482,12 @@ __device__ __forceinline__ Sums sums_outside(const DistillArgs &a, const Row<BF1
     }
     return s;
 }
-template <int NT, bool BF16, class Own>
+template <int NT, bool KEEP, bool BF16, class Own>
 __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> &row, const Entries &E, const Own &own, const DistillSlope &d, int first, int end,
                                           bool loose, Raw<BF16, STREAM_U> raw, const float (&xs)[SLOTS]) {
     constexpr int U = STREAM_U;
     for (int it = first; it < end; ++it) {
-        if (it > first) go_request<NT, false>(row, it, raw);
+        if (it > first) go_request<NT, KEEP>(row, it, raw);
         go_keep(raw);
         distill_put_go<NT, 1>(a, row, it, E, own, d, raw, xs);
     }
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(
     if (GRAD && goes > 0) go_request<NT, false>(row, 0, raw);
     float xs[SLOTS];
     s_elems(t, xs);
-    if (GRAD) grad_goes<NT>(a, row, E, OwnLeft{t}, loss_slope(a, w, t.head, R, r * a.grad_stride), 0, goes, true, raw, xs);
+    if (GRAD) grad_goes<NT, false>(a, row, E, OwnLeft{t}, loss_slope(a, w, t.head, R, r * a.grad_stride), 0, goes, true, raw, xs);
 }
 
 // What is left of a row's teacher for those who join its parts.
@@ -557,7 +557,7 @@ __host__ __device__ __forceinline__ u32 teacher_groups(int64_t n) { return (u32)
 // Sums outside S of a part of a row, after workgroups that have the rows' teachers: a multiple of the XCDs' number, so that the next launch finds a part in
 // the L2 where it was read, and the elements of S as they are left here, since it may write their gradients over them.  (The loss by the part that arrives last,
 // in one launch: 127 fp32 rows of 128,256 entries 16.7 us, 15.2 so, 30 bf16 rows 8.0 and 6.8.)
-template <bool BF16, bool GRAD>
+template <bool BF16, bool GRAD, bool KEEP>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Sums room[NT / 64];
@@ -576,7 +576,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) 
     entries_load(a, tr, G);
     entries_place<NT, U>(a, row, G, E);
     if (!has_teacher) {
-        Sums s = sums_outside<BF16, GRAD, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
+        Sums s = sums_outside<BF16, KEEP, NT>(a, row, E, first, min(first + a.part_goes, row.template goes<NT, U>()), part == 0);
         s = block_sums<false, NT>(s, a.c, room);
         if (threadIdx.x == 0) row_sums(a, r)[part] = make_float2(s.m, s.s);
     } else {
@@ -646,11 +646,11 @@ __global__ __launch_bounds__(STREAM_NT) void distill_join_kernel(DistillArgs a) 
     for (int s = 0; s < SLOTS; ++s) own.ids[s] = G.id[s];
     const RowLoss R = row_loss(a, h.t, out);
     if (part == 0 && threadIdx.x == 0) loss_store(a, r, h.t, R, loss_of(a, h.t, h.in, R));
-    grad_goes<NT>(a, row, E, own, loss_slope(a, w, h.t, R, r * a.grad_stride), first, end, part == 0, raw, xs);
+    grad_goes<NT, false>(a, row, E, own, loss_slope(a, w, h.t, R, r * a.grad_stride), first, end, part == 0, raw, xs);
 }
 
 // The gradient of a part of a row from what the loss has saved.
-template <bool BF16>
+template <bool BF16, bool KEEP>
 __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     __shared__ Teacher t;
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     Entries E;
     entries_load(a, tr, G);
     Raw<BF16, U> raw = {};
-    if (first < end) go_request<NT, false>(row, first, raw);
+    if (first < end) go_request<NT, KEEP>(row, first, raw);
     entries_place<NT, U>(a, row, G, E);
     // The logits of the entries that this wave is to store: no other stores them.
     float xs[SLOTS];
@@ -683,12 +683,12 @@ __global__ __launch_bounds__(STREAM_NT) void distill_grad_kernel(DistillArgs a) 
     if (threadIdx.x < 64) teacher_probs(a, lse, G, xs, t);
     __syncthreads();
     const Slope out = slope(tail > -INFINITY ? m : -INFINITY, l + tail, a.c, w * (t.head.P * expf(tail) + t.head.rest * expm1f(tail)), 0.f);
-    grad_goes<NT>(a, row, E, OwnLeft{t}, DistillSlope{out, slope(m, l, a.c, w * (t.head.P + t.head.rest), 0.f), w, r * a.grad_stride}, first, end, part == 0, raw, xs);
+    grad_goes<NT, KEEP>(a, row, E, OwnLeft{t}, DistillSlope{out, slope(m, l, a.c, w * (t.head.P + t.head.rest), 0.f), w, r * a.grad_stride}, first, end, part == 0, raw, xs);
 }
 
 // The gradient of log-probabilities and entropies: q_j (a + b log q_j) and, at the token, its own share.
 //     d / dx_j = 1 / T [ g_lp (1[j = y] - q_j) - g_H q_j (log q_j + H) ]
-template <bool BF16, bool ENT>
+template <bool BF16, bool ENT, bool KEEP>
 __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs a) {
     constexpr int NT = STREAM_NT, U = STREAM_U;
     const RowPart rp = row_part(blockIdx.x, a.parts);
@@ -708,7 +708,7 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
     const int end = min(first + a.part_goes, row.template goes<NT, U>());
     for (int it = first; it < end; ++it) {
         Raw<BF16, U> raw;
-        go_request<NT, false>(row, it, raw);
+        go_request<NT, KEEP>(row, it, raw);
         go_keep(raw);
         put_go<NT, 1, ENT>(row, it, k, a.grad, at, raw);
         if (it == here.go && (int)threadIdx.x == here.thread) put_elem<BF16>(a.grad, at + y, slope_at<ENT>(k, xy) + g);
@@ -756,7 +756,8 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
         }
     } else if (cut == PARTS) {
         const dim3 grid((u32)(a.n * a.parts) + teacher_groups(a.n));
-        launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, GRAD>, grid, dim3(STREAM_NT), 0, a);
+        if (GRAD || rows_keep(a.n, a.V, BF16)) launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, GRAD, true>, grid, dim3(STREAM_NT), 0, a);
+        else launch_kernel(KID_DISTILL, st, distill_part_kernel<BF16, GRAD, GRAD>, grid, dim3(STREAM_NT), 0, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if constexpr (GRAD) launch_kernel(KID_DISTILL_JOIN, st, distill_join_kernel<BF16>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
@@ -788,25 +789,30 @@ static int grad_goes_of(int64_t n, int V) {
     while (n * row_parts(V, per) > ((int64_t)1 << 24) - 1) ++per;
     return per;
 }
+template <bool BF16>
+static void launch_distill_grad(const DistillArgs &a, hipStream_t st) {
+    const dim3 grid((u32)(a.n * a.parts));
+    if (rows_keep(a.n, a.V, BF16)) launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
+    else launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
+}
 hipError_t distill_grad_launch(DistillArgs a, hipStream_t st) {
     a.part_goes = grad_goes_of(a.n, a.V);
     a.parts = row_parts(a.V, a.part_goes);
-    const dim3 grid((u32)(a.n * a.parts));
-    if (a.dtype == DT_BF16) launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<true>, grid, dim3(STREAM_NT), 0, a);
-    else launch_kernel(KID_ROWS_GRAD, st, distill_grad_kernel<false>, grid, dim3(STREAM_NT), 0, a);
+    if (a.dtype == DT_BF16) launch_distill_grad<true>(a, st);
+    else launch_distill_grad<false>(a, st);
     return hipGetLastError();
 }
-template <bool BF16>
+template <bool BF16, bool ENT>
 static void launch_logprob_grad(const LogprobGradArgs &a, hipStream_t st) {
     const dim3 grid((u32)(a.n * a.parts));
-    if (a.g_entropy) launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, true>, grid, dim3(STREAM_NT), 0, a);
-    else launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, false>, grid, dim3(STREAM_NT), 0, a);
+    if (rows_keep(a.n, a.V, BF16)) launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, ENT, true>, grid, dim3(STREAM_NT), 0, a);
+    else launch_kernel(KID_ROWS_GRAD, st, logprob_grad_kernel<BF16, ENT, false>, grid, dim3(STREAM_NT), 0, a);
 }
 hipError_t logprob_grad_launch(LogprobGradArgs a, hipStream_t st) {
     a.part_goes = grad_goes_of(a.n, a.V);
     a.parts = row_parts(a.V, a.part_goes);
-    if (a.dtype == DT_BF16) launch_logprob_grad<true>(a, st);
-    else launch_logprob_grad<false>(a, st);
+    if (a.dtype == DT_BF16) a.g_entropy ? launch_logprob_grad<true, true>(a, st) : launch_logprob_grad<true, false>(a, st);
+    else a.g_entropy ? launch_logprob_grad<false, true>(a, st) : launch_logprob_grad<false, false>(a, st);
     return hipGetLastError();
 }
 

@@ -340,7 +340,7 @@ __device__ __forceinline__ int top_of_slots(TopRoom<NT> &r, const Row<BF16> &row
 extern __shared__ __align__(16) unsigned char lp_lds[];
 
 // Whole rows.  ASK: a go is asked for while the one before is worked on.
-template <bool BF16, bool ENT, bool TOP, int NT, bool ASK>
+template <bool BF16, bool ENT, bool TOP, int NT, bool ASK, bool KEEP>
 __global__ __launch_bounds__(NT, ASK ? 4 : 8) void logprob_stream_kernel(LogprobArgs a) {
     constexpr int U = STREAM_U;
     const int64_t e = blockIdx.x;
@@ -367,10 +367,10 @@ __global__ __launch_bounds__(NT, ASK ? 4 : 8) void logprob_stream_kernel(Logprob
     const int goes = row.template goes<NT, U>();
     bool zeros = false;
     Raw<BF16, U> raw, next;
-    if (ASK && goes > 0) go_request<NT, false>(row, 0, raw);
+    if (ASK && goes > 0) go_request<NT, KEEP>(row, 0, raw);
     for (int it = 0; it < goes; ++it) {
-        if (ASK) go_request<NT, false>(row, min(it + 1, goes - 1), next);
-        else go_request<NT, false>(row, it, raw);
+        if (ASK) go_request<NT, KEEP>(row, min(it + 1, goes - 1), next);
+        else go_request<NT, KEEP>(row, it, raw);
         float x[8 * U];
         go_take<NT, U>(row, it, raw, 0, x);
         if (ASK) raw = next;
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(STREAM_NT, 8) void logprob_parts_kernel(LogprobArgs
     bool zeros = false;
     for (int it = part * a.part_goes; it < end; ++it) {
         Raw<BF16, U> raw;
-        go_request<NT, false>(row, it, raw);
+        go_request<NT, true>(row, it, raw);
         float x[8 * U];
         go_take<NT, U>(row, it, raw, 0, x);
         const float mx = max_of(x);
@@ -488,11 +488,11 @@ __global__ __launch_bounds__(STREAM_NT, 8) void logprob_parts_kernel(LogprobArgs
 
 template <bool BF16, bool ENT, bool TOP>
 static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
-    const auto whole = [&](auto nt, auto ask) {
+    const auto whole = [&](auto nt, auto ask, auto keep) {
         constexpr int NT = decltype(nt)::value;
-        constexpr bool ASK = decltype(ask)::value;
+        constexpr bool ASK = decltype(ask)::value, KEEP = decltype(keep)::value;
         const size_t goes = (a.V + NT * STREAM_U * 8 - 1) / (NT * STREAM_U * 8), lds = TOP ? sizeof(TopRoom<NT>) + goes * NT * 2 : 0;
-        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, NT, ASK>, dim3((u32)a.n), dim3(NT), lds, a);
+        launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, NT, ASK, KEEP>, dim3((u32)a.n), dim3(NT), lds, a);
     };
     switch (rows_cut(a.n, a.V, BF16, a.row_of != nullptr)) {
         case HELD:
@@ -504,9 +504,12 @@ static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
         case PARTS:
             launch_kernel(KID_LOGPROBS, st, logprob_parts_kernel<BF16, ENT, TOP>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);
             break;
-        case WIDE: whole(std::integral_constant<int, WIDE_NT>(), std::false_type()); break;
-        case AHEAD: whole(std::integral_constant<int, STREAM_NT>(), std::true_type()); break;
-        case WHOLE: whole(std::integral_constant<int, STREAM_NT>(), std::false_type()); break;
+        case WIDE:
+            if (rows_keep(a.n, a.V, BF16)) whole(std::integral_constant<int, WIDE_NT>(), std::false_type(), std::true_type());
+            else whole(std::integral_constant<int, WIDE_NT>(), std::false_type(), std::false_type());
+            break;
+        case AHEAD: whole(std::integral_constant<int, STREAM_NT>(), std::true_type(), std::false_type()); break;
+        case WHOLE: whole(std::integral_constant<int, STREAM_NT>(), std::false_type(), std::false_type()); break;
     }
     return hipGetLastError();
 }

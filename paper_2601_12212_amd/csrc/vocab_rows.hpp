@@ -75,7 +75,7 @@ struct Raw {
     static constexpr int N = U * 8 / Row<BF16>::E;
     Vec16 r[N];
 };
-// the units of go `it` of this thread; those past the end are the last unit again (row.units > 0)
+// the units of go `it` of this thread; those past the end are the last unit again (row.units > 0).  KEEP: through the caches, as other loads, or past them.
 template <int NT, bool KEEP, bool BF16, int U>
 __device__ __forceinline__ void go_request(const Row<BF16> &row, int it, Raw<BF16, U> &raw) {
 #pragma unroll
@@ -119,6 +119,11 @@ __device__ __forceinline__ void go_take(const Row<BF16> &row, int it, const Raw<
         }
     }
 }
+
+// Few logits, which the last-level cache (256 MB) is likely to hold as what has written them left them, are read through the caches; more are read past them.  Us, through |
+// past: wide 128 fp32 rows of 128,256 (66 MB) 14.7 | 17.0, of 50,001 9.9 | 10.5; loss in parts 300 fp32 rows of 50,001 15.1 | 16.0, 383 of 128,256 (196 MB) 39.7 | 36.0;
+// gradients of 100 bf16 rows of 128,256 10.0 | 11.3, 8,192 of 32,000 (524 MB) 185 | 179.  (A branch inside of all kernels costs more registers than it gives.)
+inline bool rows_keep(int64_t n, int V, bool bf16) { return n * V <= ((int64_t)64 << 20) / (bf16 ? 2 : 4); }
 
 // Between two passes over what was read: else the compiler keeps the first pass's floats, twice the registers of bf16 elements.  And before what is read is worked
 // on and stored unit by unit: all of it has arrived then.
