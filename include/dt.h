@@ -418,7 +418,7 @@ int dt_token_logprobs_grad(void *stream, int64_t n_rows, const void *logits, dt_
  * A row whose teacher_row is outside 0 .. n_teacher-1 has no teacher: loss, stats and tail 0, gradient 0.  Several rows may have the same
  * teacher.  A token that is in several entries counts with the sum of its terms.  A student's probability of 0 where the teacher has
  * some makes the loss +inf; such a row's gradient is that of the formula, with q of a row without finite entries 0.
- * The teacher's probabilities are taken in 64 bits, sums over the row are fp32, one rounding of the gradient to type t.
+ * The teacher's probabilities are taken to 2^-28 and summed in 64 bits, sums over the row are fp32, one rounding of the gradient to type t.
  * dt_distill_rows_grad is the gradient on its own, from the stats and tail that dt_distill_rows has written for the same arguments.
  * Workspace: dt_logprob_workspace_bytes(n_rows, V) bytes.
  * Errors: k < 1, fewer teacher rows than rows without teacher_row, unknown or both flags, a temperature outside 1e-4 .. 1e4, a grad that is the logits
@@ -444,8 +444,8 @@ int dt_distill_rows_grad(void *stream, int64_t n_rows, const void *logits, dt_dt
  * dt_profile_enable(0) switches it off.  dt_profile_read sums, for one kernel id
  * (0 draft row chunks, 1 row merge, 2 tree, 3 attention, 4 reserved (no launch), 5 target row
  * chunks, 6 accept, 7 dt_topk_rows chunks, 8 commit, 9 policy layer 1, 10 policy head, 11 per-node target samples,
- * 12 reward, 13 token log-probabilities, 14 distillation loss, 15 its gradient where that takes a second
- * launch, 16 gradients of rows), the elapsed milliseconds of the launches recorded
+ * 12 reward, 13 token log-probabilities, 14 distillation loss, 15 its second launch where the rows are in
+ * parts, 16 gradients of rows), the elapsed milliseconds of the launches recorded
  * since the last enable, waiting for them to finish.  Not thread-safe.
  */
 int dt_profile_enable(int max_launches);

@@ -721,22 +721,25 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
     }
 }
 
-constexpr int64_t MEET_ROWS = 3 * CUS / 2;
+constexpr int64_t MEET_ROWS = 3 * CUS / 2, HELD_ROWS = 11 * CUS / 8;
 // How rows are cut whose gradient is asked for too.  Rows of up to 131,072 bf16 entries, or half as many of fp32, fit the registers of a compute unit, a workgroup of 1,024
-// threads, which then reads them once; while it waits, though, the compute unit has nothing else.  So: with one row to a compute unit, or many, and long ones.
+// threads, which then reads them once (shorter rows too, however many: 8,000 of 21,840 138 us, whole 161); while it waits, though, the compute unit has nothing else.  So: with one row to a compute unit, or many, and long ones.
 // Loss and gradient, us, in parts | held | whole (read twice, the second time from the caches), bf16:
-//     V = 50,001:  n = 64 12.4 | 12.2 | 15.9;  200 16.8 | 12.9 | 18.0;  300 21.7 | 24.2 | 22.1;  800 48 | 49 | 43;  2,048 100 | 101 | 100
-//     V = 128,256: n = 64 13.7 | 20.0 | 30.4;  200 27.2 | 23.5 | 35.5;  300 40.4 | 43.8 | 44.2;  800 102 | 94 | 100;  2,048 246 | 198 | 246
+//     V = 50,001:  n = 64 10.0 | 12.4 | 15.9;  127 12.8 | 12.7 | -;  200 15.9 | 13.2 | 18.0;  300 20.2 | 24.5 | 22.1;  800 - | 49 | 43;  2,048 - | 101 | 100
+//     V = 128,256: n = 64 12.8 | 20.3 | 30.4;  127 18.8 | 20.8 | -;  200 28.0 | 23.5 | 35.5;  300 39.7 | 44.1 | 44.2;  383 49.1 | 46.2 | -;  800 - | 94 | 100;  2,048 - | 198 | 246
+// and fp32 rows of 50,001: n = 300 33.2 | 33.0, 383 44.3 | 35.3.
 static Cut grad_cut(int64_t n, int V, bool bf16) {
+    if (V >= HELD_LEAST && V <= HELD_V && launch_holds(n, 512)) return HELD;
     const Cut c = rows_cut(n, V, bf16, false);
     if (c == HELD || c == PARTS || V < HELD_LEAST) return c;
     const bool fits = V <= (bf16 ? 131072 : 65536);
-    if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= MEET_ROWS && launch_holds(n, 1024)))) return HELD;
+    if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= HELD_ROWS && launch_holds(n, 1024)))) return HELD;
     return n < MEET_ROWS ? PARTS : WHOLE;
 }
 // The loss alone: as log-probabilities (200 rows of 50,001 bf16 entries wide 9.5 us, in parts 10.5), but little more than one row to a compute unit in parts (300 rows of
-// 50,001 fp32 entries 15.2 us, wide 20.5, whole 20.9), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
+// 50,001 fp32 entries 15.2 us, wide 20.5, whole 20.9; of 21,840 bf16 held 9.7, 10.3), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
 static Cut loss_cut(int64_t n, int V, bool bf16) {
+    if (V > HELD_MID && V <= HELD_V && n < MEET_ROWS) return HELD;
     const Cut c = rows_cut(n, V, bf16, true);
     return c == AHEAD || (c == WIDE && n > CUS) ? n < MEET_ROWS ? PARTS : c == WIDE ? WIDE : WHOLE : c;
 }
@@ -747,8 +750,11 @@ static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {
         launch_kernel(KID_DISTILL, st, distill_held_kernel<BF16, GRAD, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
     };
     const Cut cut = GRAD ? grad_cut(a.n, a.V, BF16) : loss_cut(a.n, a.V, BF16);
-    if (cut == HELD && a.V <= HELD_V) {
-        by_held(a.V, held);
+    if (cut == HELD && a.V <= HELD_MID) {
+        by_held_mid(a.n, a.V, held);
+    } else if (cut == HELD && a.V <= HELD_V) {
+        if (a.n <= CUS) held(Held<1024, 4>());
+        else held(Held<512, 8>());
     } else if (cut == HELD) {
         if constexpr (GRAD) {
             if (a.V <= 65536) held(Held<1024, 8>());

@@ -208,9 +208,9 @@ __device__ __forceinline__ void alternatives_write(const LogprobArgs &a, int64_t
 }
 
 // ---- rows that a workgroup holds ----
-// Waves of a SIMD: as many as leave a thread its registers, but a few spilled ones with TOP (8,000 bf16 rows of 21,840, k 1: 97 us at 6, 122 at 5).
+// Waves of a SIMD: as many as leave a thread its registers, but a few spilled ones with TOP (8,000 bf16 rows of 12,000, k 1: 52 us at 6, 55 at 5).
 template <bool BF16, bool ENT, bool TOP, int NT, int U>
-__global__ __launch_bounds__(NT, !BF16 && U == 8 ? 4 : TOP ? 6 : ENT && U == 8 ? 7 : 8) void logprob_held_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(NT, NT == 1024 || (!BF16 && U == 8) ? 4 : TOP ? 6 : ENT && U == 8 ? 7 : 8) void logprob_held_kernel(LogprobArgs a) {
     constexpr int G = 2;  // units that are worked on at once: with four, registers go to scratch, and 8,000 fp32 rows of 6,000 (k 20) take 98 us for 48
     const int64_t e = blockIdx.x;
     const int tid = threadIdx.x;
@@ -494,12 +494,14 @@ static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
         const size_t goes = (a.V + NT * STREAM_U * 8 - 1) / (NT * STREAM_U * 8), lds = TOP ? sizeof(TopRoom<NT>) + goes * NT * 2 : 0;
         launch_kernel(KID_LOGPROBS, st, logprob_stream_kernel<BF16, ENT, TOP, NT, ASK, KEEP>, dim3((u32)a.n), dim3(NT), lds, a);
     };
+    const auto held = [&](auto h) {
+        constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
+        launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
+    };
     switch (rows_cut(a.n, a.V, BF16, a.row_of != nullptr)) {
         case HELD:
-            by_held(a.V, [&](auto h) {
-                constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
-                launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
-            });
+            if (a.V <= HELD_MID) by_held_mid(a.n, a.V, held);
+            else held(Held<1024, 4>());
             break;
         case PARTS:
             launch_kernel(KID_LOGPROBS, st, logprob_parts_kernel<BF16, ENT, TOP>, dim3((u32)(a.n * a.parts)), dim3(STREAM_NT), 0, a);

@@ -172,8 +172,8 @@ __device__ __forceinline__ float log2_weight(float x, float m, float c) {
     return plain_ref(M2) ? fmaf(x, c, -M2) : x == m ? 0.f : (x - m) * c;
 }
 // Elements into a thread's sums; mx: their largest.  A weight of 0 has an exponent of -inf, whose share of w is no number: where a wave
-// comes upon one (`zeros`, the same for its lanes), w is summed with the exponents held above -1e4, from there on.  (Always so it is an instruction for
-// every element: 4,096 rows of 128,256 entries 169 us.)
+// comes upon one (`zeros`, the same for its lanes), w is summed with the exponents held above -1e4, from there on.  (Always so it would be an instruction more for
+// every element.)
 template <bool ENT, int N>
 __device__ __forceinline__ void sums_add(Sums &a, const float (&x)[N], float mx, float c, bool &zeros) {
     if (mx > a.m) sums_move<ENT>(a, mx, c);
@@ -293,23 +293,28 @@ __device__ __forceinline__ void parts_leave(u64 *marks, int parts) {
 // A go of a workgroup that streams reads 8,192 elements, 16 or 32 KB; with four times the threads, four times that.
 constexpr int STREAM_NT = 256, WIDE_NT = 1024, STREAM_U = 4, STREAM_ELEMS = 8 * STREAM_NT * STREAM_U;
 inline int row_goes(int V) { return (V + STREAM_ELEMS - 1) / STREAM_ELEMS; }
-// Workgroups that hold a row in their registers: threads, and units of a thread.  f(Held<NT, U>) for a row of V entries.
+constexpr int64_t CUS = 256;
+// Workgroups that hold a row in their registers: threads, and units of a thread.  f(Held<NT, U>) for n rows of V entries.  As few threads as hold the row, but while
+// compute units have room more of them, each with less to do.  Us, less | more threads:
+//     V = 1,900:  n = 1,000 4.6 | 6.7 (log-probabilities), 7.5 | 9.8 (loss and gradient, as all second figures here), bf16
+//     V = 12,000: n = 1 4.7 | 4.6, 7.0 | 5.7;  300 6.7 | 6.4, 9.7 | 9.0;  8,000 46 | 57, 77 | 85, bf16;  n = 1 4.8 | 4.4, 7.2 | 6.0;  300 7.0 | 6.9, 10.4 | 9.4;  1,000 11.1 | 11.1, 16.9 | 20.1, fp32
+//     V = 21,840: n = 64 6.2 | 6.1, 8.4 | 8.1;  300 8.8 | 8.8, 12.6 | 12.6;  1,000 14.8 | 16.4, 21.6 | 23.9, bf16;  n = 64 6.7 | 6.1, 8.8 | 8.3;  300 9.9 | 9.9, 13.8 | 16.9, fp32
 template <int NT_, int U_>
 struct Held {
     static constexpr int NT = NT_, U = U_;
 };
+constexpr int HELD_LEAST = 32, HELD_MID = 16384, HELD_V = 32768;  // (shorter rows may have no whole unit)
 template <class F>
-inline void by_held(int V, F f) {
+inline void by_held_mid(int64_t n, int V, F f) {
     if (V <= 2048) f(Held<64, 4>());
     else if (V <= 8192) f(Held<256, 4>());
-    else if (V <= 16384) f(Held<256, 8>());
-    else f(Held<512, 8>());
+    else if (n <= 2 * CUS) f(Held<512, 4>());
+    else f(Held<256, 8>());
 }
-constexpr int HELD_LEAST = 32, HELD_V = 32768;  // (shorter rows may have no whole unit)
 // A launch has fewer than 2^32 threads.  (Rows are fewer than 2^24: only workgroups of more than 256 come there.)
 inline bool launch_holds(int64_t n, int nt) { return n * nt < (int64_t)1 << 32; }
 enum Cut {
-    HELD,   // a workgroup holds a row: one launch, read once, whatever the number of rows
+    HELD,   // a workgroup holds a row
     PARTS,  // a row is many workgroups', which meet
     WIDE,   // whole rows, 1,024 threads to each
     AHEAD,  // whole rows, 256 threads to each, a go asked for while the one before is worked on
@@ -321,13 +326,14 @@ enum Cut {
 //     V = 50,001:  n = 64 7.3 / 11.6 | 9.1 / 12.4 | - | 10.8 / 15.1;  200 9.5 / 15.8 | 9.8 / 13.1 | 8.9 / 12.6 | 11.6 / 15.5;  500 14.4 / 22.5 | 13.7 / 17.9 | 12.7 / 16.7 | 13.9 / 18.1
 //     V = 128,256: n = 64 8.8 / 14.1 | 12.1 / 15.8 | - | 20.4 / 25.2;  200 15.0 / 22.8 | 13.3 / 16.6 | 15.0 / 19.1 | 21.7 / 26.4;  500 27 / 38 | 25.9 / 28.8 | 23.8 / 27.6 | 26.3 / 31.1;
 //                  2,048 83 / 106 | 83.7 / 93.5 | 89.7 / 96.9 | 83.2 / 90.5
+// A row that a workgroup could hold, V = 21,840, held | ahead or whole: n = 300 8.8 / 13.6 | 7.6 / 11.1;  8,000 85 / 121 | 69 / 85;  V = 12,000: 300 6.7 / 10.3 | 6.6 / 9.9;  8,000 46 / 67 | 52 / 63.
 // some_none: rows that are named one by one, of which some are none.  Then the next workgroup has to take a place that is free: long rows, the emitted ones of 64
 // sequences, 281 of 576, were 24.4 us wide, where two fit a compute unit, and 30.5 by 256 threads, where those that come to a compute unit at first stay.
-constexpr int64_t PARTS_ROWS = 128, CUS = 256, MANY_ROWS = 2048;
+constexpr int64_t PARTS_ROWS = 128, MANY_ROWS = 2048;
 inline bool row_is_long(int V, bool bf16) { return (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024; }
 inline Cut rows_cut(int64_t n, int V, bool bf16, bool some_none) {
-    if (V >= HELD_LEAST && V <= HELD_V && (V <= 16384 || launch_holds(n, 512))) return HELD;
     if (V < HELD_LEAST) return WHOLE;
+    if (V <= HELD_MID || (V <= HELD_V && n <= CUS)) return HELD;
     if (n < PARTS_ROWS) return PARTS;
     if (n <= CUS || (some_none && n < MANY_ROWS && row_is_long(V, bf16))) return WIDE;
     return n <= 2 * CUS ? AHEAD : WHOLE;
