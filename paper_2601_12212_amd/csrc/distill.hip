@@ -730,7 +730,7 @@ constexpr int64_t MEET_ROWS = 3 * CUS / 2, HELD_ROWS = 11 * CUS / 8;
 // and fp32 rows of 50,001: n = 300 33.2 | 33.0, 383 44.3 | 35.3.
 static Cut grad_cut(int64_t n, int V, bool bf16) {
     if (V >= HELD_LEAST && V <= HELD_V && launch_holds(n, 512)) return HELD;
-    const Cut c = rows_cut(n, V, bf16, false);
+    const Cut c = rows_cut(n, V, bf16, false, false);
     if (c == HELD || c == PARTS || V < HELD_LEAST) return c;
     const bool fits = V <= (bf16 ? 131072 : 65536);
     if (fits && (n <= CUS || (row_is_long(V, bf16) && n >= HELD_ROWS && launch_holds(n, 1024)))) return HELD;
@@ -740,7 +740,7 @@ static Cut grad_cut(int64_t n, int V, bool bf16) {
 // 50,001 fp32 entries 15.2 us, wide 20.5, whole 20.9; of 21,840 bf16 held 9.7, 10.3), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
 static Cut loss_cut(int64_t n, int V, bool bf16) {
     if (V > HELD_MID && V <= HELD_V && n < MEET_ROWS) return HELD;
-    const Cut c = rows_cut(n, V, bf16, true);
+    const Cut c = rows_cut(n, V, bf16, true, false);
     return c == AHEAD || (c == WIDE && n > CUS) ? n < MEET_ROWS ? PARTS : c == WIDE ? WIDE : WHOLE : c;
 }
 template <bool BF16, bool GRAD>

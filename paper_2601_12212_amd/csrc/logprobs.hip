@@ -498,7 +498,7 @@ static hipError_t launch_rows(const LogprobArgs &a, hipStream_t st) {
         constexpr int NT = decltype(h)::NT, U = decltype(h)::U;
         launch_kernel(KID_LOGPROBS, st, logprob_held_kernel<BF16, ENT, TOP, NT, U>, dim3((u32)a.n), dim3(NT), 0, a);
     };
-    switch (rows_cut(a.n, a.V, BF16, a.row_of != nullptr)) {
+    switch (rows_cut(a.n, a.V, BF16, a.row_of != nullptr, TOP)) {
         case HELD:
             if (a.V <= HELD_MID) by_held_mid(a.n, a.V, held);
             else held(Held<1024, 4>());

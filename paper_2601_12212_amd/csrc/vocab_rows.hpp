@@ -327,14 +327,16 @@ enum Cut {
 //     V = 128,256: n = 64 8.8 / 14.1 | 12.1 / 15.8 | - | 20.4 / 25.2;  200 15.0 / 22.8 | 13.3 / 16.6 | 15.0 / 19.1 | 21.7 / 26.4;  500 27 / 38 | 25.9 / 28.8 | 23.8 / 27.6 | 26.3 / 31.1;
 //                  2,048 83 / 106 | 83.7 / 93.5 | 89.7 / 96.9 | 83.2 / 90.5
 // A row that a workgroup could hold, V = 21,840, held | ahead or whole: n = 300 8.8 / 13.6 | 7.6 / 11.1;  8,000 85 / 121 | 69 / 85;  V = 12,000: 300 6.7 / 10.3 | 6.6 / 9.9;  8,000 46 / 67 | 52 / 63.
+// best: alternatives are asked for, whose list the last part makes alone.  20 of them, parts | wide, V = 50,001: n = 64 12.1 | 11.4, 96 13.1 | 11.6;  128,256: 64 14.5 | 15.3, 96 16.8 | 15.4;
+// 300,001: 96 26.4 | 27.1.
 // some_none: rows that are named one by one, of which some are none.  Then the next workgroup has to take a place that is free: long rows, the emitted ones of 64
 // sequences, 281 of 576, were 24.4 us wide, where two fit a compute unit, and 30.5 by 256 threads, where those that come to a compute unit at first stay.
 constexpr int64_t PARTS_ROWS = 128, MANY_ROWS = 2048;
 inline bool row_is_long(int V, bool bf16) { return (int64_t)V * (bf16 ? 2 : 4) >= 160 * 1024; }
-inline Cut rows_cut(int64_t n, int V, bool bf16, bool some_none) {
+inline Cut rows_cut(int64_t n, int V, bool bf16, bool some_none, bool best) {
     if (V < HELD_LEAST) return WHOLE;
     if (V <= HELD_MID || (V <= HELD_V && n <= CUS)) return HELD;
-    if (n < PARTS_ROWS) return PARTS;
+    if (n < (best && V <= 1 << 18 ? 80 : PARTS_ROWS)) return PARTS;
     if (n <= CUS || (some_none && n < MANY_ROWS && row_is_long(V, bf16))) return WIDE;
     return n <= 2 * CUS ? AHEAD : WHOLE;
 }

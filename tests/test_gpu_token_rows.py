@@ -476,7 +476,8 @@ def test_a_step_says_what_it_emitted_and_what_the_draft_can_learn():
 # How rows are cut among workgroups goes by their number, length and type: one of each kind, and the edges between them.
 CUTS = [(127, 33001, 3), (128, 33001, 3), (200, 50003, 0), (256, 40001, 20), (257, 40001, 1), (300, 33001, 20), (512, 32769, 0), (513, 33003, 4),
         (600, 50001, 20), (3000, 31, 3), (100, 16384, 7), (100, 16385, 7), (90, 32768, 31),
-        (256, 20001, 5), (257, 20001, 5), (600, 30001, 0), (512, 12001, 9), (513, 12001, 9)]
+        (256, 20001, 5), (257, 20001, 5), (600, 30001, 0), (512, 12001, 9), (513, 12001, 9),
+        (79, 40001, 6), (80, 40001, 6), (90, 270001, 2), (40, 50001, 32)]
 
 
 @pytest.mark.parametrize("n, V, k", CUTS)
