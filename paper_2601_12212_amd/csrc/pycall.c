@@ -175,6 +175,7 @@ static void *whole(const dt_tensor_reader *rd, PyObject *t, const char *name, in
 static void *rows_of(const dt_tensor_reader *rd, PyObject *t, const char *name, int device, long long *s, long long *row) {
     dt_tensor_plain p;
     shape(rd, t, 2, 1, s);
+    if (!PyErr_Occurred() && s[1] > INT32_MAX) PyErr_SetString(PyExc_OverflowError, "argument does not fit an int");
     *row = stride(rd, t, 0);
     if (s[0] == 1 && *row < s[1]) *row = s[1]; /* one row: its stride says nothing */
     plain(rd, t, &p);

@@ -124,6 +124,17 @@ def test_the_binding_refuses_tensors_that_are_not_as_said(call, kw, error):
         dt.dt_token_logprobs(*_args(**kw))
 
 
+def test_the_binding_refuses_vocabularies_beyond_an_int(call):
+    """Rows of 2^32 + 50 entries are not rows of 50.  (Nothing is read of them.)"""
+    g = lambda *s, **kw: OnGpu(torch.zeros(*s, **kw))
+    long = OnGpu(torch.empty(1).as_strided((1, (1 << 32) + 50), (0, 0)))
+    long.stride = lambda dim=None: ((1 << 32) + 50, 1) if dim is None else ((1 << 32) + 50, 1)[dim]
+    with pytest.raises(OverflowError):
+        dt.dt_token_logprobs_grad(long, g(1, **i32), 1.0, g(1, 2), g(1), g(1), g(1), long)
+    with pytest.raises(OverflowError):
+        dt.dt_distill_rows(long, g(1, 5), g(1, 5, **i32), None, None, 1.0, 1, None, g(1), g(1, 2), g(1), None, None)
+
+
 def test_the_binding_refuses_tensors_of_another_device(call):
     with pytest.raises(dt.DtError) as e:                       # as said: refused for the workspace alone
         dt.dt_token_logprobs(*_args(ws=None))
