@@ -619,3 +619,42 @@ def test_students_that_are_as_good_as_certain(n, V, dtype, flags):
     ref.close(o["tail"], want["tail"], 2 * d * (1 + want["tail"].abs()), "tail")
     for name in ("grad", "again"):
         check_grad(o[name], want["grad"], scale * want["size"], dtype, V, (flags, name))
+
+
+@pytest.mark.parametrize("n", [1, 33, 130])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_largest_vocabulary(n, dtype):
+    """DT_VOCAB_MAX entries, the most alternatives, the most teacher's entries."""
+    V, k = dt.DT_VOCAB_MAX, 32
+    g = torch.Generator().manual_seed(n)
+    some = torch.unique(torch.tensor([0, n // 2, n - 1]))
+    x = (torch.randn(len(some), V, generator=g) * 3).to(dtype)
+    xd = (torch.randn(n, V, device=DEV) * 2).to(dtype)
+    xd[some.to(DEV)] = x.to(DEV)
+    tokens = torch.full((n,), V - 1, **i32)
+    got = run_logprobs(xd[None], None, tokens.to(DEV)[None], 1.0, k, n)
+    check_logprobs({name: v[:, some.to(DEV)] for name, v in got.items()}, x, tokens[some], 1.0, k)
+    val, ids, lse = teacher(len(some), V, 128, n, short=False)
+    m = torch.full((n,), -1, **i32)
+    m[some] = torch.arange(len(some), **i32)
+    o = run_distill(xd, val, ids, lse, m, 1.0, 1, None, True)
+    want = ref.distill(x, val, ids, lse, None, 1.0, 1)
+    check_distill({name: v[some.to(DEV)] for name, v in o.items()}, want, dtype, V)
+    o = run_distill(xd, val, ids, lse, m, 1.0, 1, None, False)
+    check_distill({name: v[some.to(DEV)] for name, v in o.items()}, want, dtype, V)
+
+
+@pytest.mark.parametrize("n, V", [(1, 524288), (5, 50001), (79, 40001), (127, 33001), (300, 33001), (383, 40001), (40, 300001)])
+def test_workspaces_hold_what_is_left_in_them(n, V):
+    """What lies behind the bytes that were asked for stays as it was."""
+    x = torch.randn(n, V, device=DEV).to(BF16)
+    size = dt.dt_logprob_workspace_bytes(n, V)
+    room = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    ws = room[:size]
+    o = dict(st=dirty(1, n, 2), tl=dirty(1, n, 32), ti=dirty(1, n, 32, dtype=torch.int32))
+    dt.dt_token_logprobs(x[None], None, None, 1.0, 32, None, None, o["st"], o["tl"], o["ti"], ws)
+    val, ids = torch.full((n, 128), -6.0, device=DEV), torch.arange(128, dtype=torch.int32, device=DEV).repeat(n, 1)
+    for grad in (None, torch.empty_like(x)):
+        dt.dt_distill_rows(x, val, ids, None, None, 1.0, 1, None, dirty(n), dirty(n, 2), dirty(n), grad, ws)
+    torch.cuda.synchronize()
+    assert (room[size:] == 0x5A).all()
