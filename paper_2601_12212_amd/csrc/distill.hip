@@ -110,6 +110,7 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
         p[s] = lp[s] = 0.0;
+        if (s && a.k <= 64 * s) break;  // uniform, as below: what is not there is not even fetched
         if (G.id[s] >= 0) {
             const float v = G.val[s], hi = v - lse, back = hi - v;
             lp[s] = (double)v - (double)lse;
@@ -132,12 +133,13 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
     bool first[SLOTS], twice = false;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
+        first[s] = G.id[s] >= 0;
+        if (s && a.k <= 64 * s) break;
         t.id[64 * s + lane] = G.id[s];
         t.p[64 * s + lane] = p[s];
         t.lp[64 * s + lane] = lp[s];
         t.sum[64 * s + lane] = (float)p[s];
         t.x[64 * s + lane] = x[s];
-        first[s] = G.id[s] >= 0;
     }
     wave_sync();
     // Every entry writes its number to a place that its id names; who finds another's there has the same id, or only the same place, and tries another.
@@ -181,8 +183,10 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
     // the student's elements of S, one for each id
     Sums in = {-INFINITY, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s)
+    for (int s = 0; s < SLOTS; ++s) {
+        if (s && a.k <= 64 * s) break;
         if (first[s]) sums_add1<false>(in, x[s], a.c);
+    }
     wave_sums<false>(in, a.c);
     if (lane == 0) {
         t.head = TeacherHead{(float)P, (a.flags & DT_DISTILL_TAIL) ? (float)fmax(0.0, 1.0 - P) : 0.f, in.m, in.s};
@@ -248,6 +252,7 @@ __device__ __forceinline__ void loss_write(const DistillArgs &a, int64_t r, cons
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
         const int i = 64 * s + lane_id();
+        if (s && a.k <= 64 * s) break;
         const double p = t.p[i];
         if (p > 0.0) term += p * (t.lp[i] - (double)log_prob(t.x[i], R.st, a.c));
     }
@@ -260,6 +265,7 @@ __device__ __forceinline__ double loss_in(const DistillArgs &a, const Teacher &t
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
         const int i = 64 * s + lane_id();
+        if (s && a.k <= 64 * s) break;
         const double p = t.p[i];
         if (p > 0.0) term += p * (t.lp[i] - (t.head.in_m > -INFINITY ? ((double)t.x[i] - (double)t.head.in_m) * (double)(a.c * LN2) : -INFINITY));
     }
