@@ -125,10 +125,21 @@ def special_rows(V, dtype):
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("many", [False, True], ids=["few", "many"])
 def test_logprobs_of_special_rows(V, dtype, many):
+    check_special_rows(V, dtype, 2048 if many else 1)    # more rows than are cut into parts
+
+
+@pytest.mark.parametrize("V", [12000, 20000, 40000])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("at_least", [1, 140, 300, 600])
+def test_logprobs_of_special_rows_by_their_number(V, dtype, at_least):
+    check_special_rows(V, dtype, at_least)
+
+
+def check_special_rows(V, dtype, at_least):
     named = special_rows(V, dtype)
     x = torch.stack(list(named.values()))
     n = len(x)
-    reps = 2048 // n + 1 if many else 1                  # more rows than are cut into parts
+    reps = (at_least - 1) // n + 1
     tokens = torch.full((n,), V // 2, **i32)
     xd = put(x.repeat(reps, 1))
     got = run_logprobs(xd[None], None, tokens.repeat(reps).to(DEV)[None], 1.0, 32, n * reps)
@@ -658,3 +669,22 @@ def test_workspaces_hold_what_is_left_in_them(n, V):
         dt.dt_distill_rows(x, val, ids, None, None, 1.0, 1, None, dirty(n), dirty(n, 2), dirty(n), grad, ws)
     torch.cuda.synchronize()
     assert (room[size:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("n, V", [(1, 12000), (140, 20000), (7, 40000), (140, 40000), (300, 40000), (600, 20000)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_best_of_rows_whose_best_are_neighbours_or_far_apart(n, V, dtype):
+    """The k best all in one thread's elements, in one go, in the first and last places, one to a go; ties at the k-th."""
+    k = 20
+    g = torch.Generator().manual_seed(V + n)
+    base = (torch.randn(V, generator=g)).to(dtype)
+    places = [torch.arange(k) + V // 2, torch.arange(k) * (V // k), torch.cat([torch.arange(k // 2), torch.arange(V - k // 2, V)]), torch.arange(k) * 8 + 3,
+              torch.arange(k + 40) * 100, torch.randperm(V, generator=g)[:k]]
+    x = torch.stack([base] * len(places))
+    for r, at in enumerate(places):
+        x[r, at] = (10.0 + torch.arange(len(at)) // 2 * 0.25).to(dtype) if r != 4 else torch.tensor(9.0, dtype=dtype)
+    reps = (n - 1) // len(x) + 1
+    got = run_logprobs(put(x.repeat(reps, 1), 1, 3)[None], None, None, 1.0, k, reps * len(x))
+    want = ref.logprobs(x, torch.zeros(len(x), **i32), 1.0, k)
+    ids = got["top_id"][0].cpu().view(reps, len(x), k)
+    assert torch.equal(ids, want["top_id"][None].expand_as(ids))
