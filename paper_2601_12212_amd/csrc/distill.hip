@@ -746,8 +746,10 @@ static Cut grad_cut(int64_t n, int V, bool bf16) {
 // 50,001 fp32 entries 15.2 us, wide 20.5, whole 20.9; of 21,840 bf16 held 9.7, 10.3), and long rows wide (1,200 of 128,256 bf16 52 us, whole 54).
 static Cut loss_cut(int64_t n, int V, bool bf16) {
     if (V > HELD_MID && V <= HELD_V && n < MEET_ROWS) return HELD;
-    const Cut c = rows_cut(n, V, bf16, true, false);
-    return c == AHEAD || (c == WIDE && n > CUS) ? n < MEET_ROWS ? PARTS : c == WIDE ? WIDE : WHOLE : c;
+    const Cut c = rows_cut(n, V, bf16, false, false);
+    if (c == HELD || c == PARTS || V < HELD_LEAST) return c;
+    if (n > CUS && n < MEET_ROWS) return PARTS;
+    return n <= CUS || (row_is_long(V, bf16) && n < MANY_ROWS) ? WIDE : WHOLE;
 }
 template <bool BF16, bool GRAD>
 static hipError_t launch_distill(const DistillArgs &a, hipStream_t st) {

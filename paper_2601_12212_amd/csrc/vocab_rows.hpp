@@ -320,15 +320,16 @@ enum Cut {
     AHEAD,  // whole rows, 256 threads to each, a go asked for while the one before is worked on
     WHOLE   // whole rows, 256 threads to each
 };
-// Rows that are streamed: few are cut, so that they fill the chip; with one row to a compute unit 1,024 threads read it; with two, 256 threads that ask ahead;
+// Rows that are streamed: few are cut, so that they fill the chip; with one row to a compute unit 1,024 threads read it, if it is long; with two, 256 threads that ask ahead;
 // beyond that rows are there by the thousand, and eight small workgroups to a compute unit overlap one's end with another's reading, with as few registers as that takes.
+// Alternatives (best) are listed by a row's last part alone, so that parts end earlier.
 // Log-probabilities of n rows of V bf16 entries, us, with no / 20 alternatives, parts | wide | ahead | whole:
-//     V = 50,001:  n = 64 7.3 / 11.6 | 9.1 / 12.4 | - | 10.8 / 15.1;  200 9.5 / 15.8 | 9.8 / 13.1 | 8.9 / 12.6 | 11.6 / 15.5;  500 14.4 / 22.5 | 13.7 / 17.9 | 12.7 / 16.7 | 13.9 / 18.1
-//     V = 128,256: n = 64 8.8 / 14.1 | 12.1 / 15.8 | - | 20.4 / 25.2;  200 15.0 / 22.8 | 13.3 / 16.6 | 15.0 / 19.1 | 21.7 / 26.4;  500 27 / 38 | 25.9 / 28.8 | 23.8 / 27.6 | 26.3 / 31.1;
-//                  2,048 83 / 106 | 83.7 / 93.5 | 89.7 / 96.9 | 83.2 / 90.5
+//     V = 50,001:  n = 64 6.7 / 10.8 | 7.8 / 10.3 | 8.5 / 11.4 | 8.3 / 13.9;  96 7.6 / 11.9 | 8.0 / 10.6 | 8.8 / 11.4 | 11.0 / 14.2;  127 8.3 / 13.0 | 8.8 / 11.3 | 8.9 / 11.6 | 10.9 / 14.2;
+//                  200 9.8 / 15.1 | 9.7 / 12.3 | 9.2 / 11.8 | 11.5 / 14.6;  500 13.8 / 21.0 | 15.3 / 18.4 | 12.5 / 15.8 | 13.8 / 17.3
+//     V = 128,256: n = 64 8.5 / 12.8 | 11.4 / 14.2 | 14.7 / 17.6 | 20.4 / 24.1;  96 10.2 / 15.0 | 11.6 / 14.6 | 14.9 / 17.7 | 20.7 / 24.6;  127 12.2 / 17.3 | 11.8 / 14.9 | 15.0 / 17.7 | 21.1 / 24.9;
+//                  200 15.0 / 21.4 | 12.6 / 15.6 | 15.4 / 18.4 | 21.7 / 25.4;  500 28.6 / 37.3 | 25.0 / 27.7 | 23.5 / 26.7 | 26.1 / 30.1;  2,048 83 / 106 | 84 / 93 | 90 / 97 | 83 / 90
+//     V = 250,001: n = 96 13.3 / 21.7 | 19.1 / 22.6;  127 15.5 / 24.9 | 19.5 / 22.9
 // A row that a workgroup could hold, V = 21,840, held | ahead or whole: n = 300 8.8 / 13.6 | 7.6 / 11.1;  8,000 85 / 121 | 69 / 85;  V = 12,000: 300 6.7 / 10.3 | 6.6 / 9.9;  8,000 46 / 67 | 52 / 63.
-// best: alternatives are asked for, whose list the last part makes alone.  20 of them, parts | wide, V = 50,001: n = 64 12.1 | 11.4, 96 13.1 | 11.6;  128,256: 64 14.5 | 15.3, 96 16.8 | 15.4;
-// 300,001: 96 26.4 | 27.1.
 // some_none: rows that are named one by one, of which some are none.  Then the next workgroup has to take a place that is free: long rows, the emitted ones of 64
 // sequences, 281 of 576, were 24.4 us wide, where two fit a compute unit, and 30.5 by 256 threads, where those that come to a compute unit at first stay.
 constexpr int64_t PARTS_ROWS = 128, MANY_ROWS = 2048;
@@ -337,7 +338,7 @@ inline Cut rows_cut(int64_t n, int V, bool bf16, bool some_none, bool best) {
     if (V < HELD_LEAST) return WHOLE;
     if (V <= HELD_MID || (V <= HELD_V && n <= CUS)) return HELD;
     if (n < (best && V <= 1 << 18 ? 80 : PARTS_ROWS)) return PARTS;
-    if (n <= CUS || (some_none && n < MANY_ROWS && row_is_long(V, bf16))) return WIDE;
+    if (n <= (row_is_long(V, bf16) ? some_none ? MANY_ROWS - 1 : CUS : 5 * CUS / 8)) return WIDE;
     return n <= 2 * CUS ? AHEAD : WHOLE;
 }
 // goes of a part, so that there are about eight workgroups to a compute unit; parts of a row (up to 64)

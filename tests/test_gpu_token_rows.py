@@ -488,7 +488,7 @@ def test_a_step_says_what_it_emitted_and_what_the_draft_can_learn():
 CUTS = [(127, 33001, 3), (128, 33001, 3), (200, 50003, 0), (256, 40001, 20), (257, 40001, 1), (300, 33001, 20), (512, 32769, 0), (513, 33003, 4),
         (600, 50001, 20), (3000, 31, 3), (100, 16384, 7), (100, 16385, 7), (90, 32768, 31),
         (256, 20001, 5), (257, 20001, 5), (600, 30001, 0), (512, 12001, 9), (513, 12001, 9),
-        (79, 40001, 6), (80, 40001, 6), (90, 270001, 2), (40, 50001, 32)]
+        (79, 40001, 6), (80, 40001, 6), (160, 40001, 6), (161, 40001, 6), (256, 90001, 6), (90, 270001, 2), (40, 50001, 32)]
 
 
 @pytest.mark.parametrize("n, V, k", CUTS)
@@ -534,7 +534,7 @@ def test_more_entries_than_a_launch_of_large_workgroups_has():
 
 
 DISTILL_CUTS = [(127, 33001), (130, 33001), (130, 65536), (130, 70001), (256, 40001), (257, 40001), (300, 33001), (383, 32769), (384, 33003), (400, 41001),
-                (400, 82001), (90, 32768), (90, 16385), (256, 20001), (257, 20001), (383, 16400), (400, 30001), (512, 12001), (513, 12001), (352, 82001)]
+                (400, 82001), (90, 32768), (90, 16385), (256, 20001), (257, 20001), (383, 16400), (400, 30001), (161, 40001), (512, 12001), (513, 12001), (352, 82001)]
 
 
 @pytest.mark.parametrize("n, V", DISTILL_CUTS)
