@@ -410,7 +410,7 @@ int dt_token_logprobs_grad(void *stream, int64_t n_rows, const void *logits, dt_
  *   loss[r] = sum_i p_i (log p_i - log q_i)                                    (forward Kullback-Leibler divergence)
  *     DT_DISTILL_TAIL    + p_t (log p_t - log q_t), p_t = max(0, 1 - P), q_t = sum of q outside S: what the teacher gives to
  *                          all other tokens together
- *     DT_DISTILL_RENORM  with p_i / P in the place of p_i                        (not both)
+ *     DT_DISTILL_RENORM  with p_i / P in the place of p_i, whatever values all entries share (teacher_lse too)   (not both)
  *   stats [n_rows, 2]  as in dt_token_logprobs
  *   tail  [n_rows]     log q_t
  *   grad  [n_rows, grad_stride], may be NULL: type t, grad_loss[r] (NULL: 1) times the gradient of loss[r] in the logits; its rows may be the

@@ -106,6 +106,13 @@ __device__ __forceinline__ double exp_pair(float hi, float lo) {
 // By one wave: the entries into `t`; x: the student's logits.
 __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, const Given &G, const float (&x)[SLOTS], Teacher &t) {
     const int lane = lane_id();
+    const bool renorm = a.flags & DT_DISTILL_RENORM;
+    if (renorm) {  // p_i / P does not depend on what all values share, and with the largest taken off nothing leaves the exponential's range that counts
+        float most = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) most = fmaxf(most, G.id[s] >= 0 ? G.val[s] : -INFINITY);
+        lse = wave_max(most);
+    }
     double P = 0.0, p[SLOTS], lp[SLOTS];
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -119,7 +126,7 @@ __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, c
         }
     }
     P = wave_sum_f64(P);
-    if ((a.flags & DT_DISTILL_RENORM) && P > 0.0) {
+    if (renorm && P > 0.0) {  // (1 to DT_DISTILL_K_MAX: the largest of them is 1)
         const float l0 = logf((float)P);
         const double l = (double)l0 + (P * exp_pair(-l0, 0.f) - 1.0);
 #pragma unroll
