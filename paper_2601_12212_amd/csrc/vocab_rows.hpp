@@ -214,7 +214,8 @@ __device__ __forceinline__ void sums_add(Sums &a, const float (&x)[N], float mx,
 }
 template <bool ENT>
 __device__ __forceinline__ void sums_add1(Sums &a, float x, float c) {
-    sums_join<ENT>(a, Sums{x, x == -INFINITY ? 0.f : 1.f, 0.f}, c);
+    const float t = -ref_off(x, c), e = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t);  // (not 1: a sum is against M2, and so is what is read off it)
+    sums_join<ENT>(a, Sums{x, e, ENT ? e * t : 0.f}, c);
 }
 // (v_max3_f32 by name: fmaxf makes every element a quiet number first, an instruction each)
 __device__ __forceinline__ float max3(float a, float b, float c) {

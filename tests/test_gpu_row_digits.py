@@ -63,3 +63,59 @@ def test_renorm_of_entries_next_to_nothing():
     o = run_distill(xd, val, ids, None, None, 1.0, dt.DT_DISTILL_RENORM, None, True)
     check_distill(o, want, F32, V)
     assert float(o["loss"][2]) == 0.0 and (o["grad"][2] == 0).all()
+
+
+# ---- rows with one token that has all of the weight: its log-probability and the log of the sum are 0
+
+def _places(V, dtype):
+    """Ends of the row, and of its units, goes and parts wherever its address puts them."""
+    unit = 8 if dtype == BF16 else 4
+    at = {0, 1, 2, 3, 7, unit, unit + 1, V // 2, V - 1, V - 2, V - 3, V - unit, V - unit - 1}
+    for edge in (2048, 8192, 16384, 32768):
+        at |= {edge - 1, edge, edge + unit - 1, edge + 7}
+    return sorted(a for a in at if 0 <= a < V)
+
+
+@pytest.mark.parametrize("n, V", CUTS)
+@pytest.mark.parametrize("dtype", [BF16, F32], **IDS)
+@pytest.mark.parametrize("T", [1.0, 0.01, 1e-4])
+@pytest.mark.parametrize("hidden", [True, False], ids=["masked", "far below"])
+def test_a_certain_token_anywhere_in_its_row(n, V, dtype, T, hidden):
+    """A row's other tokens are -inf, or too far below to count.  The weight is 2^r with |r| <= 2^-4, a rounding's; its exponential is off by one step (2 u) and so is
+    the logarithm of that (2 u / ln 2 of a power, times ln 2): 4 u in all."""
+    places = _places(V, dtype)
+    n = max(n, len(places))
+    g = torch.Generator().manual_seed(V)
+    at = torch.tensor(places).repeat((n - 1) // len(places) + 1)[:n]
+    value = (10.0 + 30.0 * torch.rand(n, generator=g)).to(dtype)
+    x = (torch.full((n, V), -math.inf) if hidden else torch.randn(n, V, generator=g) - 200.0).to(dtype)
+    x[torch.arange(n), at] = value
+    for offset, pad in ((0, 0), (3, 1)):
+        got = run_logprobs(put(x, offset, pad)[None], None, at.int().to(DEV)[None], T, 1, n)
+        assert (got["logprob"].abs() <= 4 * U).all(), float(got["logprob"].abs().max())
+        assert (got["stats"][0, :, 1].abs() <= 4 * U).all(), float(got["stats"][0, :, 1].abs().max())
+        assert torch.equal(got["stats"][0, :, 0].cpu(), value.float())
+        assert torch.equal(got["top_id"][0, :, 0].cpu(), at.int()) and (got["top_logprob"].abs() <= 4 * U).all()
+        assert (got["entropy"].abs() <= 8 * U).all()       # log s - w / s: two terms of up to 2^-4, each off by a few of its steps
+
+
+@pytest.mark.parametrize("n, V", CUTS + [(400, 70001)])
+@pytest.mark.parametrize("dtype", [BF16, F32], **IDS)
+@pytest.mark.parametrize("T", [1.0, 0.01, 1e-4])
+def test_a_certain_token_among_the_teachers_entries_or_outside(n, V, dtype, T):
+    """The certain token in S: the loss is log p of it (p = 1 here: 0), and outside S nothing.  Outside S: log q_t is 0, and so is the loss of a teacher that
+    gives all to that outside."""
+    g = torch.Generator().manual_seed(V)
+    at = torch.tensor(_places(V, dtype)).repeat(n)[:n]
+    x = torch.full((n, V), -math.inf).to(dtype)
+    value = (10.0 + 30.0 * torch.rand(n, generator=g)).to(dtype)
+    x[torch.arange(n), at] = value
+    xd = put(x, 1, 1)
+    o = run_distill(xd, torch.zeros(n, 1), at.int()[:, None], None, None, T, 0, None, True)
+    assert (o["loss"].abs() <= 4 * U).all(), float(o["loss"].abs().max())
+    assert (o["stats"][:, 1].abs() <= 4 * U).all() and (o["tail"] == -math.inf).all()
+    # d = (q_j - 1) / T at the token, of which q_j is a sum's quotient (4 u) or from the saved logarithm
+    for name in ("grad", "again"):
+        assert (o[name].double().abs().amax(1) <= 8 * U / T).all(), name
+    o = run_distill(xd, torch.full((n, 1), -1e5), ((at + 1) % V).int()[:, None], None, None, T, dt.DT_DISTILL_TAIL, None, False)
+    assert (o["loss"].abs() <= 8 * U).all() and (o["tail"].abs() <= 4 * U).all(), float(o["tail"].abs().max())
