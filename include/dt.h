@@ -418,7 +418,7 @@ int dt_token_logprobs_grad(void *stream, int64_t n_rows, const void *logits, dt_
  * A row whose teacher_row is outside 0 .. n_teacher-1 has no teacher: loss, stats and tail 0, gradient 0.  Several rows may have the same
  * teacher.  A token that is in several entries counts with the sum of its terms.  A student's probability of 0 where the teacher has
  * some makes the loss +inf; such a row's gradient is that of the formula, with q of a row without finite entries 0.
- * The teacher's probabilities are taken to 2^-28 and summed in 64 bits, sums over the row are fp32, one rounding of the gradient to type t.
+ * The teacher's probabilities are taken to 2^-40 and summed in 64 bits, sums over the row are fp32, one rounding of the gradient to type t.
  * dt_distill_rows_grad is the gradient on its own, from the stats and tail that dt_distill_rows has written for the same arguments.
  * Workspace: dt_logprob_workspace_bytes(n_rows, V) bytes.
  * Errors: k < 1, fewer teacher rows than rows without teacher_row, unknown or both flags, a temperature outside 1e-4 .. 1e4, a grad that is the logits

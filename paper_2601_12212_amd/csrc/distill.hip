@@ -14,6 +14,8 @@
 
 #include "vocab_rows.hpp"
 
+#include "exp_pair.hpp"
+
 namespace dt {
 
 // ---- the teacher's entries for a row ----
@@ -83,26 +85,6 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 __device__ __forceinline__ double wave_sum_f64(double v) { return readlane_f64(wave_scan_incl_f64(v), 63); }
-// exp(hi + lo) to about 2^-28, since 1 - P is one of the teacher's probabilities: e^g for g = hi + lo - n ln 2, |g| <= 0.35, as
-// 1 + g + g^2 (1/2 + g (1/6 + ...)), the sum of the first two exact.  (In 64 bits the function's constants alone, two registers each, were kept by every
-// thread for as long as its row.)
-__device__ __forceinline__ double exp_pair(float hi, float lo) {
-    if (!(hi > -104.f)) return 0.0;
-    const float n = rintf(hi * LOG2E);
-    // n ln 2 in three parts, the first two of so few digits that their products are exact
-    const float a = fmaf(n, -0.693359375f, hi), b = n * 2.12194440e-4f;  // ln 2 = 0.693359375 - 2.12194440e-4 + 1.646595e-12
-    const float c = fmaf(n, -1.646595e-12f, lo);
-    float g = a + b;
-    const float bb = g - a, e0 = (a - (g - bb)) + (b - bb);  // a + b = g + e0
-    const float low = e0 + c, v = g + low;
-    float q = fmaf(v, 1.9841270e-4f, 1.3888889e-3f);
-    q = fmaf(v, q, 8.3333333e-3f);
-    q = fmaf(v, q, 4.1666667e-2f);
-    q = fmaf(v, q, 1.6666667e-1f);
-    q = fmaf(v, q, 0.5f);
-    q = v * v * q;
-    return ldexp(1.0 + (double)g + ((double)low + (double)q), (int)n);
-}
 // By one wave: the entries into `t`; x: the student's logits.
 __device__ __forceinline__ void teacher_probs(const DistillArgs &a, float lse, const Given &G, const float (&x)[SLOTS], Teacher &t) {
     const int lane = lane_id();
@@ -421,8 +403,10 @@ __device__ __forceinline__ void s_elems(const Row<BF16> &row, const Given &G, fl
 }
 
 // ---- rows that a workgroup holds: read once ----
+// Waves of a SIMD: as many as leave a thread its registers (the loss alone of 300 bf16 rows of 20,001 by 512 threads: 10.3 us at 8 with two in scratch, 9.7 at 7; of 8,000 of 12,001 by
+// 256 47.9 at 8 with four in scratch, 48.2 at 7).
 template <bool BF16, bool GRAD, int NT, int U>
-__global__ __launch_bounds__(NT, NT == 1024 ? 4 : NT == 64 ? 5 : BF16 ? (GRAD ? 7 : 8) : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
+__global__ __launch_bounds__(NT, NT == 1024 ? 4 : NT == 64 ? 5 : BF16 ? (GRAD || NT * U == 4096 ? 7 : 8) : U == 4 ? 6 : 4) void distill_held_kernel(DistillArgs a) {
     constexpr int G = 2;  // units that are worked on at once: 8,000 bf16 rows of 6,000 with the gradient in 48 us, 54 with four
     __shared__ Teacher t;
     __shared__ Sums room[NT / 64];

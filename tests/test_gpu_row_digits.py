@@ -119,3 +119,31 @@ def test_a_certain_token_among_the_teachers_entries_or_outside(n, V, dtype, T):
         assert (o[name].double().abs().amax(1) <= 8 * U / T).all(), name
     o = run_distill(xd, torch.full((n, 1), -1e5), ((at + 1) % V).int()[:, None], None, None, T, dt.DT_DISTILL_TAIL, None, False)
     assert (o["loss"].abs() <= 8 * U).all() and (o["tail"].abs() <= 4 * U).all(), float(o["tail"].abs().max())
+
+
+# ---- the teacher's probabilities
+
+@pytest.mark.parametrize("n, V", CUTS[:-2])
+@pytest.mark.parametrize("left", [1e-4, 1e-6])
+def test_what_a_teacher_that_is_nearly_certain_gives_to_other_tokens(n, V, left):
+    """p_t = 1 - P where it is small: it is known to 2^-40 / p_t, so that the gradient outside S, which is p_t q_j / q_t for a student that is surer still, has
+    the digits of others of its size."""
+    k = 3
+    g = torch.Generator().manual_seed(V)
+    p = torch.rand(n, k, generator=g, dtype=torch.float64) * 0.2 + 0.2
+    p[:, 0] += 0.3
+    p = p / p.sum(1, keepdim=True) * (1 - left * (1 + torch.rand(n, 1, generator=g, dtype=torch.float64)))
+    lse = torch.randn(n, generator=g) * 10
+    val = (torch.log(p) + lse.double()[:, None]).float()
+    P = torch.exp(val.double() - lse.double()[:, None]).sum(1)
+    # (rounding val moves P by up to 2^-20: where that is more than what is to be left, the largest entry is lowered until it is not)
+    while (1 - P < left).any():
+        val[:, 0] = torch.where(1 - P < left, torch.nextafter(val[:, 0], torch.tensor(-math.inf)), val[:, 0])
+        P = torch.exp(val.double() - lse.double()[:, None]).sum(1)
+    ids = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(n)]).int()
+    x = (torch.randn(n, V, generator=g) - 40.0).scatter(1, ids.long(), torch.rand(n, k, generator=g))
+    some = torch.unique(torch.tensor([0, 1, n // 2, n - 1]))
+    want = ref.distill(x[some], val[some], ids[some], lse[some], None, 1.0, 1)
+    o = run_distill(put(x, 1, 1), val, ids, lse, None, 1.0, 1, None, True)
+    assert (want["tail"] < -25).all()
+    check_distill({name: v[some.to(DEV)] for name, v in o.items()}, want, F32, V)
