@@ -147,3 +147,26 @@ def test_what_a_teacher_that_is_nearly_certain_gives_to_other_tokens(n, V, left)
     o = run_distill(put(x, 1, 1), val, ids, lse, None, 1.0, 1, None, True)
     assert (want["tail"] < -25).all()
     check_distill({name: v[some.to(DEV)] for name, v in o.items()}, want, F32, V)
+
+
+# ---- the gradient in fp32
+
+@pytest.mark.parametrize("n, V", [(2, 1000), (2, 2047), (3, 8003), (3, 13001), (5, 20011), (3, 50021), (3, 131071), (140, 33001), (140, 50021), (400, 66001), (600, 20011), (3, 19)])
+@pytest.mark.parametrize("half", [False, True], ids=["all", "half of them masked"])
+def test_gradients_of_equal_logits_have_fp32s_digits(n, V, half):
+    """Logits 0 or -inf: every weight is 1 and every sum exact, so q = 1 / count to half a step, and the gradient outside S, P q, has P's rounding and those of q_t,
+    P q_t, the sums' quotient (two) and the weight's product: 8 u at most; in S, (P q - p), three more, relative to both terms."""
+    k = 2
+    x = torch.zeros(n, V)
+    if half:
+        x[:, 1::2] = -math.inf
+    ids = torch.stack([torch.arange(n) % 3 * 2, torch.full((n,), V - 1 - (V - 1) % 2)], 1).int()
+    val = torch.log(torch.tensor([[0.3, 0.4]])).expand(n, k).contiguous()
+    p = torch.exp(val.double())
+    q = torch.where(x == 0, 1.0 / (x == 0).sum(1, keepdim=True).double(), 0.0).double()
+    want = p.sum(1, keepdim=True) * q
+    size = want.clone()
+    want = want.scatter_add(1, ids.long(), -p)
+    size = size.scatter_add(1, ids.long(), p)
+    o = run_distill(put(x, 1, 1), val, ids, None, None, 1.0, 0, None, True)
+    ref.close(o["grad"], want, 8 * U * size)
