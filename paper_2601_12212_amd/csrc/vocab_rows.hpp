@@ -272,7 +272,9 @@ __device__ __forceinline__ RowStat row_stat(float m, float s, float c) {
     return r;
 }
 __device__ __forceinline__ float log_prob(float x, const RowStat &r, float c) {
-    return r.m == -INFINITY ? -INFINITY : (log2_weight(x, r.m, c) - r.log2s) * LN2;
+    const float t = log2_weight(x, r.m, c);
+    // (a logit next to the type's lowest leaves fp32's range times log2(e), and may not without)
+    return r.m == -INFINITY ? -INFINITY : t > -INFINITY ? (t - r.log2s) * LN2 : (x - r.m) * (c * LN2);
 }
 
 // ---- parts of a row that meet in their own launch ----------------------------------------------------

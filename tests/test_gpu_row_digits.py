@@ -170,3 +170,36 @@ def test_gradients_of_equal_logits_have_fp32s_digits(n, V, half):
     size = size.scatter_add(1, ids.long(), p)
     o = run_distill(put(x, 1, 1), val, ids, None, None, 1.0, 0, None, True)
     ref.close(o["grad"], want, 8 * U * size)
+
+
+# ---- tokens that are masked by their type's lowest value
+
+@pytest.mark.parametrize("n, V", CUTS)
+@pytest.mark.parametrize("dtype", [BF16, F32], **IDS)
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_tokens_masked_by_the_lowest_value(n, V, dtype, T):
+    """Their logits are finite, and so are their log-probabilities, (lowest - m) / T: four roundings, those of log2(e) / T, ln 2, their product and the last."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.full((n, V), LOWEST[dtype])
+    open_ = torch.stack([torch.randperm(V, generator=g)[:3] for _ in range(n)])
+    x = x.scatter(1, open_, torch.randn(n, 3, generator=g)).to(dtype)
+    masked = (open_[:, 0] + 1) % V
+    while True:
+        inside = (open_ == masked[:, None]).any(1)
+        if not inside.any():
+            break
+        masked = torch.where(inside, (masked + 1) % V, masked)
+    k = min(V, 5)
+    some = torch.unique(torch.tensor([0, n // 2, n - 1]))
+    want = ref.logprobs(x[some], masked[some].int(), T, k)
+    assert torch.isfinite(want["logprob"]).all() and (want["logprob"] < -1e38).all()
+    got = run_logprobs(put(x, 1, 1)[None], None, masked.int().to(DEV)[None], T, k, n)
+    assert torch.equal(got["top_id"][0, some.to(DEV)].cpu(), want["top_id"])
+    size = lambda v: ref.delta(V) + 6 * U * v.abs()
+    ref.close(got["logprob"][0, some.to(DEV)], want["logprob"], size(want["logprob"]))
+    ref.close(got["top_logprob"][0, some.to(DEV)], want["top_logprob"], size(want["top_logprob"]))
+    # a teacher that gives such a token half of its weight: a loss of half of that
+    val, ids = torch.full((n, 1), math.log(0.5)), masked.int()[:, None]
+    for with_grad in (True, False):
+        o = run_distill(put(x, 1, 1), val, ids, None, None, T, 0, None, with_grad)
+        ref.close(o["loss"][some.to(DEV)], -0.5 * want["logprob"], 8 * U * want["logprob"].abs())
