@@ -193,8 +193,8 @@ __device__ __forceinline__ Slope slope(float m, float l, float c, float a, float
 }
 // a q of an element against a sum that is at hand: the factor's quotient by the sum, and not the sum's logarithm, whose roundings would be in every gradient of the row (up to
 // 6e-7 of each in fp32 rows of 50,001).
-__device__ __forceinline__ Slope slope_by_sum(float m, float s, float c, float a) {
-    return s > 0.f ? Slope{m, ref_off(m, c), c, a / s, 0.f} : Slope{0.f, INFINITY, c, a, 0.f};
+__device__ __forceinline__ Slope slope_by_sum(float m, float part, float c, float a) {
+    return part > 0.f ? Slope{m, ref_off(m, c), c, a * part, 0.f} : Slope{0.f, INFINITY, c, a, 0.f};
 }
 // What the gradients of a row with a teacher go by.  Outside S the gradient is q_j (P - p_t (1 - q_t) / q_t): q_j / q_t, which the sums outside S give, times
 // P q_t - p_t q_in with q_in = 1 - q_t, a sum of its own.  Neither factor leaves fp32's range, and where a student is near its teacher only
@@ -207,7 +207,7 @@ struct DistillSlope {
 // From the row's sums in S and outside, by any thread.
 struct RowLoss {
     RowStat st;
-    float whole;        // sum over all tokens, against st.m
+    float part;         // 1 / the sum over all tokens, against st.m
     float q_in, q_out;  // of the student
     Sums out;
 };
@@ -219,14 +219,14 @@ __device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const TeacherH
     const float whole = in.s + o.s, part = whole > 0.f ? 1.f / whole : 0.f;
     RowLoss R;
     R.st = row_stat(m, whole, a.c);
-    R.whole = whole;
+    R.part = part;
     R.q_in = in.s * part;
     R.q_out = o.s * part;
     R.out = out;
     return R;
 }
 __device__ __forceinline__ DistillSlope loss_slope(const DistillArgs &a, float w, const TeacherHead &t, const RowLoss &R, int64_t at) {
-    return DistillSlope{slope_by_sum(R.out.m, R.out.s, a.c, w * (t.P * R.q_out - t.rest * R.q_in)), slope_by_sum(R.st.m, R.whole, a.c, w * (t.P + t.rest)), w, at};
+    return DistillSlope{slope_by_sum(R.out.m, R.out.s > 0.f ? 1.f / R.out.s : 0.f, a.c, w * (t.P * R.q_out - t.rest * R.q_in)), slope_by_sum(R.st.m, R.part, a.c, w * (t.P + t.rest)), w, at};
 }
 // (a sum outside S that is nothing beside the largest logit still has a logarithm)
 __device__ __forceinline__ float log_outside(const DistillArgs &a, const RowLoss &R) {
