@@ -139,6 +139,8 @@ class Step:
         pairs of the two models' answers to the same tokens that a step leaves behind.  Rows that belong to no node of the tree have loss 0.  grad
         [total_rows, V], if given, takes the gradient in draft_logits, weighted by grad_loss [total_rows].
         -> loss [total_rows], overwritten by the next call with the same k."""
+        if k < 1:
+            raise B.DtError("dt_distill_rows", -1)
         Bz, TC, dev = self.Bsz, self.TT_cap, self.device
         node = torch.arange(TC, dtype=torch.int32, device=dev).expand(Bz, TC)
         live = node < self.n_nodes[:, None]
@@ -160,6 +162,8 @@ class Step:
         return d["loss"]
 
     def _row_buffers(self, key, n, k):
+        if k < 0:
+            raise B.DtError("dt_token_logprobs", -1)
         b = self._buffers.get(key)
         if b is None:
             f32 = dict(dtype=torch.float32, device=self.device)
