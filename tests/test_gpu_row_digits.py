@@ -10,8 +10,7 @@ torch = pytest.importorskip("torch")
 
 import paper_2601_12212_amd as dt  # noqa: E402
 from tests import _token_rows as ref  # noqa: E402
-from tests.test_gpu_token_rows import (BF16, DEV, F32, LOWEST, check_distill, i32, put, rows, run_distill, run_logprobs,  # noqa: E402
-                                       teacher)
+from tests.test_gpu_token_rows import (BF16, DEV, F32, LOWEST, check_distill, i32, put, rows, run_distill, run_logprobs, special_rows, teacher)  # noqa: E402
 
 U = ref.U
 IDS = dict(ids=["bf16", "f32"])
@@ -203,3 +202,85 @@ def test_tokens_masked_by_the_lowest_value(n, V, dtype, T):
     for with_grad in (True, False):
         o = run_distill(put(x, 1, 1), val, ids, None, None, T, 0, None, with_grad)
         ref.close(o["loss"][some.to(DEV)], -0.5 * want["logprob"], 8 * U * want["logprob"].abs())
+
+
+# ---- sums that nothing may be missing from
+
+@pytest.mark.parametrize("n, V", CUTS + [(40, 300007), (300, 30001), (300, 33001), (400, 70001), (130, dt.DT_VOCAB_MAX)])
+@pytest.mark.parametrize("dtype", [BF16, F32], **IDS)
+@pytest.mark.parametrize("half", [False, True], ids=["all", "half of them masked"])
+def test_sums_of_equal_logits_count_every_token(n, V, dtype, half):
+    """Logits 0 or -inf: the sum is their number exactly (below 2^24), so that its logarithm is off by a step of its own, by log2's (one of 1.44 times that), and by the
+    constant's and the product's: 6 u of it; the entropy is the same.  A unit of four tokens too few of 524,288 is 128 u, of 80 that are allowed there."""
+    for offset, pad in ((0, 0), (3, 1)):
+        room = torch.zeros(offset + n * (V + pad) + 8, dtype=dtype, device=DEV)
+        xd = room[offset:offset + n * (V + pad)].view(n, V + pad)[:, :V]
+        if half:
+            xd[:, 1::2] = -math.inf
+        count = (V + 1) // 2 if half else V
+        tokens = torch.full((n,), (V - 1) // 2 * 2, **i32)
+        got = run_logprobs(xd[None], None, tokens.to(DEV)[None], 1.0, 2, n)
+        log = math.log(count)
+        for name, want in (("logprob", -log), ("entropy", log), ("top_logprob", -log)):
+            assert ((got[name].double() - want).abs() <= 6 * U * log).all(), (name, float((got[name].double() - want).abs().max()) / U)
+        assert ((got["stats"][0, :, 1].double() - log).abs() <= 6 * U * log).all()
+        # the teacher's k tokens taken out: log(1 - k / count), which log1p takes of k / count (a half step, and two of its own), or two logarithms
+        k = min(3, (count - 1) // 2)
+        ids = (torch.arange(k) * 2)[None].expand(n, k).int().contiguous()
+        o = run_distill(xd, torch.full((n, k), math.log(0.25)), ids, None, None, 1.0, 0, None, False)
+        rest = math.log1p(-k / count)
+        assert ((o["tail"].double() - rest).abs() <= 6 * U * abs(rest)).all(), float((o["tail"].double() - rest).abs().max() / U)
+        assert ((o["stats"][:, 1].double() - log).abs() <= 6 * U * log).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], **IDS)
+def test_distill_of_128_rows(dtype):
+    """The first number of long rows that are not in parts."""
+    n, V, k, T = 128, 33001, 9, 1.3
+    x, xd = rows(n, V, dtype, 5, offset=3, pad=1)
+    val, ids, lse = teacher(n, V, k, 6)
+    w = torch.rand(n, generator=torch.Generator().manual_seed(n))
+    some = torch.tensor([0, 1, 2, 64, 127])
+    want = ref.distill(x[some], val[some], ids[some], lse[some], None, T, 1, w[some])
+    pick = lambda o: {name: v[some.to(DEV)] for name, v in o.items()}
+    check_distill(pick(run_distill(xd, val, ids, lse, None, T, 1, w, True)), want, dtype, V)
+    check_distill(pick(run_distill(xd, val, ids, lse, None, T, 1, None, False)), want, dtype, V)
+    same = put(x, 3, 1)
+    check_distill(pick(run_distill(same, val, ids, lse, None, T, 1, w, True, grad=same)), want, dtype, V)
+
+
+@pytest.mark.parametrize("V", [41, 5003, 40009])
+@pytest.mark.parametrize("dtype", [BF16, F32], **IDS)
+@pytest.mark.parametrize("offset, pad, reps", [(1, 0, 1), (3, 2, 1), (5, 1, 1), (6, 3, 9), (7, 0, 17)])
+def test_special_rows_at_any_address(V, dtype, offset, pad, reps):
+    """Masks, ties and extremes where rows do not start with a unit, and at every part of a row's ends."""
+    named = {name: v for name, v in special_rows(V, dtype).items() if not name.startswith(("large", "very"))}
+    x = torch.stack(list(named.values())).roll(offset, 1)
+    n = len(x)
+    tokens = torch.full((n,), V - 2, **i32)
+    want = ref.logprobs(x, tokens, 1.0, 20)
+    got = run_logprobs(put(x.repeat(reps, 1), offset, pad)[None], None, tokens.repeat(reps).to(DEV)[None], 1.0, 20, n * reps)
+    ids = got["top_id"][0].cpu().view(reps, n, 20)
+    assert torch.equal(ids, want["top_id"].expand_as(ids))
+    d = ref.delta(V) * (1 + 330.0 / 32)                   # |x| up to 330, or masked: (x - m) is rounded relative to itself
+    size = lambda v: d + 6 * U * torch.where(torch.isfinite(v), v.abs(), 0.0)
+    for name, tol in (("logprob", size(want["logprob"])), ("entropy", 2 * d * (1 + want["entropy"])), ("top_logprob", size(want["top_logprob"])), ("stats", d)):
+        for part in got[name][0].reshape((reps, n) + tuple(want[name].shape[1:]))[::4]:
+            ref.close(part, want[name], tol, name)
+
+
+@pytest.mark.parametrize("n, V", [(700, 1001), (140, 50021)])
+def test_gradients_in_bf16_are_the_fp32_ones_to_the_nearest(n, V):
+    """Logits 0: all sums are exact, in both types the same, and so are the gradients but for bf16's one rounding."""
+    g = torch.Generator().manual_seed(n)
+    w, val = torch.randn(n, generator=g), torch.log(torch.rand(n, 2, generator=g) * 0.4 + 0.05)
+    ids = torch.stack([torch.arange(n) % V, (torch.arange(n) + V // 2) % V], 1).int()
+    out = {}
+    for dtype in (F32, BF16):
+        o = run_distill(torch.zeros(n, V, dtype=dtype, device=DEV), val, ids, None, None, 1.0, 1, w, True)
+        tokens, stats = ids[:, 0].contiguous().to(DEV), o["stats"]
+        lp = torch.empty(n, V, dtype=dtype, device=DEV)
+        dt.dt_token_logprobs_grad(torch.zeros(n, V, dtype=dtype, device=DEV), tokens, 1.0, stats, stats[:, 1].contiguous(), w.to(DEV), val[:, 0].contiguous().to(DEV), lp)
+        out[dtype] = (o["grad"], o["again"], lp)
+    for a, b in zip(out[F32], out[BF16]):
+        assert torch.equal(a.to(BF16), b)
