@@ -418,6 +418,8 @@ int dt_token_logprobs_grad(void *stream, int64_t n_rows, const void *logits, dt_
  * A row whose teacher_row is outside 0 .. n_teacher-1 has no teacher: loss, stats and tail 0, gradient 0.  Several rows may have the same
  * teacher.  A token that is in several entries counts with the sum of its terms.  A student's probability of 0 where the teacher has
  * some makes the loss +inf; such a row's gradient is that of the formula, with q of a row without finite entries 0.
+ * (p_t is what rounded values leave of 1.  Where the entries are all tokens that have a probability, that may be 10^-8 and not 0, and a student that gives nothing to others then has a
+ * loss of +inf; such entries are for DT_DISTILL_RENORM.)
  * The teacher's probabilities are taken to 2^-40 and summed in 64 bits, sums over the row are fp32, one rounding of the gradient to type t.
  * dt_distill_rows_grad is the gradient on its own, from the stats and tail that dt_distill_rows has written for the same arguments.
  * Workspace: dt_logprob_workspace_bytes(n_rows, V) bytes.

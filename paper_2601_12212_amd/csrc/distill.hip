@@ -500,7 +500,8 @@ __device__ __forceinline__ void grad_goes(const DistillArgs &a, const Row<BF16> 
     }
 }
 
-// Whole rows, and their gradient in a second pass over the row, which the caches then hold.
+// Whole rows, and their gradient in a second pass over the row: from behind the L2s, which do not hold the rows of all
+// workgroups (600 fp32 rows of 66,001: 309 MB are fetched for 158; 83 us, where the bytes once in and once out are 50).
 template <bool BF16, bool GRAD, int NT>
 __global__ __launch_bounds__(NT, NT == 1024 ? 8 : 7) void distill_stream_kernel(DistillArgs a) {
     constexpr int U = STREAM_U;
@@ -558,7 +559,7 @@ __device__ __forceinline__ Sums parts_sums(const DistillArgs &a, int64_t r) {
 }
 __host__ __device__ __forceinline__ u32 teacher_groups(int64_t n) { return (u32)(n + 7) & ~7u; }
 // Sums outside S of a part of a row, after workgroups that have the rows' teachers: a multiple of the XCDs' number, so that the next launch finds a part in
-// the L2 where it was read, and the elements of S as they are left here, since it may write their gradients over them.  (The loss by the part that arrives last,
+// the L2 where it was read (51 rows of 128,256 with the gradient 12.0 us, 13.8 if the next launch is three XCDs off), and the elements of S as they are left here, since it may write their gradients over them.  (The loss by the part that arrives last,
 // in one launch: 127 fp32 rows of 128,256 entries 16.7 us, 15.2 so, 30 bf16 rows 8.0 and 6.8.)
 template <bool BF16, bool GRAD, bool KEEP>
 __global__ __launch_bounds__(STREAM_NT) void distill_part_kernel(DistillArgs a) {
@@ -727,7 +728,7 @@ __global__ __launch_bounds__(STREAM_NT) void logprob_grad_kernel(LogprobGradArgs
 constexpr int64_t MEET_ROWS = 3 * CUS / 2, HELD_ROWS = 11 * CUS / 8;
 // How rows are cut whose gradient is asked for too.  Rows of up to 131,072 bf16 entries, or half as many of fp32, fit the registers of a compute unit, a workgroup of 1,024
 // threads, which then reads them once (shorter rows too, however many: 8,000 of 21,840 138 us, whole 161); while it waits, though, the compute unit has nothing else.  So: with one row to a compute unit, or many, and long ones.
-// Loss and gradient, us, in parts | held | whole (read twice, the second time from the caches), bf16:
+// Loss and gradient, us, in parts | held | whole (read twice), bf16:
 //     V = 50,001:  n = 64 10.0 | 12.4 | 15.9;  127 12.8 | 12.7 | -;  200 15.9 | 13.2 | 18.0;  300 20.2 | 24.5 | 22.1;  800 - | 49 | 43;  2,048 - | 101 | 100
 //     V = 128,256: n = 64 12.8 | 20.3 | 30.4;  127 18.8 | 20.8 | -;  200 28.0 | 23.5 | 35.5;  300 39.7 | 44.1 | 44.2;  383 49.1 | 46.2 | -;  800 - | 94 | 100;  2,048 - | 198 | 246
 // and fp32 rows of 50,001: n = 300 33.2 | 33.0, 383 44.3 | 35.3.
